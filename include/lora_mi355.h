@@ -53,7 +53,10 @@ typedef enum {
     LORA_ERR_HIP = 8,              /* a HIP runtime call failed (no device, bad stream, ...) */
     LORA_ERR_ID_RANGE = 9,         /* adapter id outside [0, max_adapter_id] */
     LORA_ERR_STARVATION = 10,      /* lora_place_adapters: no starvation-free allocation on the GPUs given */
-    LORA_ERR_SCRATCH_LIMIT = 11    /* lora_layer_forward_static: the call needs more scratch than the static buffer holds */
+    LORA_ERR_SCRATCH_LIMIT = 11,   /* lora_layer_forward_static: the call needs more scratch than the static buffer holds */
+    LORA_ERR_KV_REFUSED = 12,      /* reported by lora_kv_poll_flags: a request or token named something that does not exist */
+    LORA_ERR_KV_EXHAUSTED = 13,    /* reported by lora_kv_poll_flags: the cache had no block left for a request */
+    LORA_ERR_NOT_FINITE = 14       /* reported by lora_kv_poll_flags: a key or value on its way into the cache was not finite */
 } lora_status;
 
 /* Segment-map modes (lora_bucket). */
@@ -424,6 +427,169 @@ lora_status lora_place_adapters(int32_t n_adapters, const int32_t *size, const d
 /* The priority order alone (paper Sec. 7, PrioritySorting): order_out[k] = index of the k-th adapter to place.
  * Errors: INVALID_ARG. */
 lora_status lora_priority_sorting(int32_t n_adapters, const int32_t *size, const double *rate, int32_t *order_out);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Between q|k|v and o of a decoder layer: a key/value cache held in four bits, its block tables, the norm and
+ * rotation of queries and keys, and attention over the cache.  What the adapters of a GPU do not take is what the
+ * cache can have (paper Sec. 2.1: the keys and values of every running request are kept; Sec. 5.1.1: resident adapters
+ * take their memory); four bits a value leave most of it to adapters.
+ *
+ * The cache is a pool of blocks of LORA_KV_BLOCK tokens, shared by the sequences and the same for every layer: block b
+ * of a sequence's row of the block table holds tokens 64 b .. 64 b + 63 of it, in every layer's own memory.  One step:
+ *
+ *     lora_kv_extend     once: blocks for the step's new tokens, and where each token goes      (beside lora_bucket)
+ *     per layer: q|k|v   lora_layer_forward_group
+ *       lora_kv_store    norm and rotation of q and k; keys and values rounded to four bits into the cache
+ *       lora_kv_attend   attention of the step's tokens, one-token requests and prompt chunks alike
+ *     o, gate|up, down   lora_layer_forward ...
+ *     lora_kv_release    when sequences end
+ *
+ * Four bits.  32 values of a head that follow each other share an exponent e: the smallest with max|x| <= 7 * 2^e, at
+ * least -100 and at most 125 (a group of zeros: -100).  Each is stored as a sign and the nearest of {0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6} * 2^e, ties to the magnitude of the even code, larger ones as 6 * 2^e.  A value is off by at most half a step: 2^e / 4
+ * below 2^e * 2, 2^e / 2 below 2^e * 4, 2^e above.  A value that is a NaN is stored as 0, an infinity like the largest finite
+ * value, and LORA_KV_FLAG_NOT_FINITE is set: the cache holds finite numbers only, so that nothing leaks out of tokens
+ * that a query does not see.
+ *
+ * Streams.  Calls on one cache share its tables and scratch.  As with a lora_ctx, a call whose stream differs from the
+ * previous call's is ordered behind it with an event.  While a stream is being captured no event is recorded or waited
+ * for, and replays are outside the library: the caller orders a capture and each of its replays with the other calls
+ * on that cache (two graphs of one cache must not run at the same time).  A captured call reads the lengths, rows and
+ * tables that are there when it is replayed, but keeps T, n and max_new of the capture; rows of the step behind a
+ * captured T are left alone.
+ * ------------------------------------------------------------------------------------------------------------- */
+#define LORA_KV_BLOCK 64
+
+typedef struct lora_kv lora_kv; /* opaque */
+
+typedef struct {
+    int32_t n_layers;       /* decoder layers, 1 .. 256 */
+    int32_t n_heads;        /* query heads, a multiple of n_kv_heads, at most 1024 */
+    int32_t n_kv_heads;     /* key (and value) heads; query head h reads key head h / (n_heads / n_kv_heads) */
+    int32_t head_dim;       /* 64 or 128 */
+    int32_t n_blocks;       /* blocks of the pool, 1 .. 2^20 */
+    int32_t max_seqs;       /* rows of the block table, 1 .. 8192 */
+    int32_t max_seq_tokens; /* longest sequence, 1 .. 2^24; max_seqs rows of that length must stay below 2^31 blocks */
+    int32_t max_tokens;     /* largest T of any step, 1 .. 2^20 */
+    void *slab;             /* device memory owned by the caller, 256-byte aligned, lora_kv_slab_bytes() long; must outlive
+                               the cache */
+    size_t slab_bytes;
+} lora_kv_config;
+
+/* Bits of the device flag word (lora_kv_poll_flags). */
+enum {
+    LORA_KV_FLAG_REFUSED = 1u,    /* lora_kv_extend / release / read met a request or token that it refuses */
+    LORA_KV_FLAG_EXHAUSTED = 2u,  /* lora_kv_extend had too few free blocks for a request */
+    LORA_KV_FLAG_NOT_FINITE = 4u  /* lora_kv_store met a NaN or an infinity in a key or value */
+};
+
+/* Result of lora_kv_extend: device memory owned by the cache, valid until the next lora_kv_extend or lora_kv_release on it.
+ * start[n + 1]: the token rows of request i are start[i] .. start[i + 1] - 1;  position[t], slot[t]: position of token row t in
+ * its sequence and its place in the cache, 64 * block + position % 64 (both -1 where the request was refused; unspecified
+ * for rows >= start[n]);  table[max_seqs][row_blocks], -1 behind a row's blocks;  held[max_seqs]: blocks of each row. */
+typedef struct {
+    const int32_t *start;
+    const int32_t *position;
+    const int32_t *slot;
+    const int32_t *table;
+    const int32_t *held;
+    int32_t row_blocks;     /* max_seq_tokens / 64, rounded up */
+    int32_t n;
+    int32_t T;
+    uint64_t epoch;         /* identifies the lora_kv_extend call that made this step */
+} lora_kv_step;
+
+/* Device bytes the cache needs for `cfg` (blocks, tables, scratch); 0 if cfg is invalid.  A block of a layer takes
+ * n_kv_heads * 68 * head_dim bytes: 4.25 bits a value. */
+size_t lora_kv_slab_bytes(const lora_kv_config *cfg);
+
+/* Creates an empty cache on the current device (paper Sec. 2.1).  Sets the whole cache to zero and waits for it.
+ * Calls on one cache are not thread-safe.  Errors: INVALID_ARG (null, out of range, misaligned slab), SHAPE (heads,
+ * head_dim), OOM (slab too small), HIP. */
+lora_status lora_kv_create(const lora_kv_config *cfg, lora_kv **out);
+
+/* Waits for the device and ends the cache; the slab stays the caller's.  Errors: INVALID_ARG (NULL). */
+lora_status lora_kv_destroy(lora_kv *kv);
+
+/* Blocks and places for the new tokens of a step (paper Sec. 2.1: prompts' tokens and one-token requests run in one
+ * step).  Request i continues the sequence in row d_seq[i] of the block table, which has d_len[i] tokens in the cache, by
+ * d_new[i] tokens; its token rows follow those of request i - 1 in the step's T rows.  Where the row holds fewer than
+ * ceil((d_len[i] + d_new[i]) / 64) blocks it gets more: the lowest free ones, request after request.  Blocks that a row
+ * holds beyond that stay its own, so that calling again with the same lengths changes nothing.  The lengths are the
+ * caller's: nothing is counted up here.  d_seq, d_len, d_new: device int32[n] (may be NULL for n = 0).
+ * T: token rows of the step; the sum of d_new may be smaller (a padded batch: rows behind the last request are left as
+ * they are by every call), not larger.  max_new: no request has more new tokens than this (T does).
+ * The result is unique.  A request is refused (LORA_KV_FLAG_REFUSED; it changes nothing, its rows are marked) when its
+ * row does not exist or an earlier request of the step has it, a length is negative, d_new exceeds max_new, the
+ * sequence would exceed max_seq_tokens, d_len is not covered by blocks that the row holds, or its rows do not fit T.  Free
+ * blocks are handed out in order until a request does not get all that it needs: it and all later requests that
+ * need one get none and are refused (LORA_KV_FLAG_EXHAUSTED).
+ * Errors: INVALID_ARG (n or T out of range, max_new < 0, null pointers), HIP. */
+lora_status lora_kv_extend(lora_kv *kv, int32_t n, const int32_t *d_seq, const int32_t *d_len, const int32_t *d_new, int32_t T,
+                           int32_t max_new, lora_kv_step *out, void *stream);
+
+/* Gives the blocks of n rows back to the pool, apart from those that hold the first d_keep[i] tokens (d_keep NULL: none are
+ * kept; a sequence that has ended, or proposed tokens that were rejected).  The same row may be named more than
+ * once.  A row that does not exist or a negative d_keep sets LORA_KV_FLAG_REFUSED and changes nothing.  The step of
+ * the latest lora_kv_extend ends with it.  Errors: INVALID_ARG, HIP. */
+lora_status lora_kv_release(lora_kv *kv, int32_t n, const int32_t *d_seq, const int32_t *d_keep, void *stream);
+
+/* Operands of the norm and rotation of heads.  Everything is bf16 with the values of a head next to each other and the
+ * heads of a token next to each other; strides count elements from token to token (0: dense; multiples of 8, at
+ * least the heads' width), pointers are 16-byte aligned.  Norm (where there is a weight): u = x / sqrt(mean(x^2) + eps) * w over
+ * each head.  Rotation (where d_inv_freq is given): the pair p = 0 .. head_dim / 2 - 1 turns by the angle position *
+ * d_inv_freq[p], taken in 64 bits.  One rounding of the result. */
+typedef struct {
+    const void *d_q, *d_k, *d_v;
+    int64_t q_stride, k_stride, v_stride;
+    void *d_q_out, *d_k_out;          /* may be d_q / d_k themselves (with their stride); otherwise not overlapping anything */
+    int64_t q_out_stride, k_out_stride;
+    const void *d_q_norm, *d_k_norm;  /* bf16 [head_dim] or NULL */
+    float eps;                        /* >= 0 */
+    const float *d_inv_freq;          /* fp32 [head_dim / 2] or NULL */
+    int32_t pairing;                  /* LORA_ROTATE_* */
+} lora_heads;
+enum {
+    LORA_ROTATE_HALVES = 0,     /* pair p: values p and p + head_dim / 2 of a head */
+    LORA_ROTATE_NEIGHBOURS = 1  /* pair p: values 2 p and 2 p + 1 */
+};
+
+/* Norm and rotation of queries and keys, on the current device: d_q [T, n_heads * head_dim] and d_k [T, n_kv_heads *
+ * head_dim] (either may be NULL, then its output too), d_position: device int32[T] (may be NULL without rotation).
+ * What lora_kv_store does for a cache, for programs that keep theirs elsewhere.  d_v must be NULL.
+ * Errors: INVALID_ARG (null or misaligned pointers, strides, eps, pairing, T < 0), SHAPE (heads, head_dim), HIP. */
+lora_status lora_head_norm_rotate(int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t *d_position,
+                                  const lora_heads *heads, void *stream);
+
+/* A layer's keys and values of the step into the cache: d_k normed and rotated at the step's positions and rounded to four
+ * bits (from fp32; computed in fp64 up to there, so that the codes do not hang on the order of a sum), d_v rounded to
+ * four bits.  In the same pass d_q (may be NULL) is normed and rotated into d_q_out; rows of a refused request get
+ * zeros there.  d_k_out must be NULL.  step: the latest of lora_kv_extend.
+ * Errors: INVALID_ARG (layer, stale step, null or misaligned pointers, strides, eps, pairing), HIP. */
+lora_status lora_kv_store(lora_kv *kv, int32_t layer, const lora_kv_step *step, const lora_heads *heads, void *stream);
+
+/* Attention of the step's tokens over a layer of the cache: out[t, h] = sum_k softmax_k(scale * q[t, h] . key[k]) value[k] over the
+ * keys k <= position[t] of the token's sequence (its own among them: lora_kv_store comes first).  d_q: bf16 [T, n_heads *
+ * head_dim], normed and rotated; d_out: the same shape, not d_q; strides as in lora_heads.  Products of bf16 queries with the exact
+ * values that the codes stand for, fp32 sums; the weights of the softmax are rounded to bf16 in front of the second product,
+ * their sum is not; one rounding of the result.  Rows of a refused request are set to zero, rows behind the last
+ * request are left as they are.  The result does not depend on what else the step holds beyond the order of fp32
+ * sums, and is the same from call to call.
+ * Errors: INVALID_ARG (layer, stale step, null or misaligned pointers, strides, scale not finite), HIP. */
+lora_status lora_kv_attend(lora_kv *kv, int32_t layer, const lora_kv_step *step, float scale, const void *d_q, int64_t q_stride,
+                           void *d_out, int64_t out_stride, void *stream);
+
+/* n tokens out of a layer of the cache, as the bf16 values that their codes stand for (to move a sequence, or to look at
+ * it): token d_position[i] of the sequence in row d_seq[i] goes to row i of d_k_out and d_v_out [n, n_kv_heads * head_dim], 16-byte
+ * aligned, either may be NULL.  A token outside of the row's blocks sets LORA_KV_FLAG_REFUSED and reads as zeros.  Needs no step.
+ * Errors: INVALID_ARG, HIP. */
+lora_status lora_kv_read(lora_kv *kv, int32_t layer, int32_t n, const int32_t *d_seq, const int32_t *d_position, void *d_k_out,
+                         void *d_v_out, void *stream);
+
+/* Blocking read-and-clear of the cache's flag word (synchronises `stream`).  Returns LORA_ERR_KV_REFUSED, LORA_ERR_KV_EXHAUSTED or
+ * LORA_ERR_NOT_FINITE for the lowest bit that was set, else LORA_OK; *flags (may be NULL) receives the raw word.  Errors:
+ * INVALID_ARG (also while the stream is being captured), HIP. */
+lora_status lora_kv_poll_flags(lora_kv *kv, uint32_t *flags, void *stream);
 
 const char *lora_status_string(lora_status s);
 

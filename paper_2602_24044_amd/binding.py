@@ -53,6 +53,9 @@ LORA_ERR_HIP = 8
 LORA_ERR_ID_RANGE = 9
 LORA_ERR_STARVATION = 10
 LORA_ERR_SCRATCH_LIMIT = 11
+LORA_ERR_KV_REFUSED = 12
+LORA_ERR_KV_EXHAUSTED = 13
+LORA_ERR_NOT_FINITE = 14
 LORA_BUCKET_SORTED = 0
 LORA_BUCKET_RUNS = 1
 LORA_PATH_AUTO = 0
@@ -61,6 +64,12 @@ LORA_PATH_SPLITK = 2
 LORA_FLAG_NOT_RESIDENT = 1
 LORA_FLAG_INTERNAL = 2
 LORA_CREATE_HOST_ONLY = 1
+LORA_KV_BLOCK = 64
+LORA_KV_FLAG_REFUSED = 1
+LORA_KV_FLAG_EXHAUSTED = 2
+LORA_KV_FLAG_NOT_FINITE = 4
+LORA_ROTATE_HALVES = 0
+LORA_ROTATE_NEIGHBOURS = 1
 
 EXPORTS = [
     "lora_slab_bytes", "lora_create", "lora_destroy", "lora_slots_load", "lora_bucket", "lora_layer_forward",
@@ -68,6 +77,8 @@ EXPORTS = [
     "lora_layer_forward_glu", "lora_model_forward_glu", "lora_poll_device_flags", "lora_slot_of", "lora_slot_adapter", "lora_slot_first_page", "lora_last_launches",
     "lora_profile_enable", "lora_profile_collect", "lora_profile_reset", "lora_status_string",
     "lora_last_hip_error", "lora_calibrate_stream", "lora_calibrate_mfma", "lora_layer_forward_static", "lora_static_scratch_bytes", "lora_set_tuning", "lora_set_bias", "lora_model_forward_group", "lora_place_adapters", "lora_priority_sorting",
+    "lora_kv_slab_bytes", "lora_kv_create", "lora_kv_destroy", "lora_kv_extend", "lora_kv_release", "lora_head_norm_rotate",
+    "lora_kv_store", "lora_kv_attend", "lora_kv_read", "lora_kv_poll_flags",
 ]
 LORA_TUNE_FUSED_VARIANT = 0
 LORA_TUNE_SPLIT_VARIANT = 1
@@ -431,3 +442,116 @@ def lora_calibrate_mfma(workgroups: int, iters: int, d_sink: int, d_ticks: int, 
 
 def lora_profile_reset(ctx: int) -> None:
     _lib.lora_profile_reset(_P(ctx))
+
+
+# ---- key/value cache in four bits ----
+class lora_kv_config(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("max_seqs", ctypes.c_int32),
+                ("max_seq_tokens", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("slab", ctypes.c_void_p),
+                ("slab_bytes", ctypes.c_size_t)]
+
+
+class lora_kv_step(ctypes.Structure):
+    _fields_ = [("start", ctypes.c_void_p), ("position", ctypes.c_void_p), ("slot", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("held", ctypes.c_void_p), ("row_blocks", ctypes.c_int32),
+                ("n", ctypes.c_int32), ("T", ctypes.c_int32), ("epoch", ctypes.c_uint64)]
+
+
+class lora_heads(ctypes.Structure):
+    _fields_ = [("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("d_q_out", ctypes.c_void_p), ("d_k_out", ctypes.c_void_p),
+                ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
+                ("d_q_norm", ctypes.c_void_p), ("d_k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("d_inv_freq", ctypes.c_void_p), ("pairing", ctypes.c_int32)]
+
+
+_KVC, _KVS, _KVH = ctypes.POINTER(lora_kv_config), ctypes.POINTER(lora_kv_step), ctypes.POINTER(lora_heads)
+_lib.lora_kv_slab_bytes.restype = ctypes.c_size_t
+_lib.lora_kv_slab_bytes.argtypes = [_KVC]
+_lib.lora_kv_create.restype = ctypes.c_int
+_lib.lora_kv_create.argtypes = [_KVC, ctypes.POINTER(_P)]
+_lib.lora_kv_destroy.restype = ctypes.c_int
+_lib.lora_kv_destroy.argtypes = [_P]
+_lib.lora_kv_extend.restype = ctypes.c_int
+_lib.lora_kv_extend.argtypes = [_P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, ctypes.c_int32, _KVS, _P]
+_lib.lora_kv_release.restype = ctypes.c_int
+_lib.lora_kv_release.argtypes = [_P, ctypes.c_int32, _P, _P, _P]
+_lib.lora_head_norm_rotate.restype = ctypes.c_int
+_lib.lora_head_norm_rotate.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _KVH, _P]
+_lib.lora_kv_store.restype = ctypes.c_int
+_lib.lora_kv_store.argtypes = [_P, ctypes.c_int32, _KVS, _KVH, _P]
+_lib.lora_kv_attend.restype = ctypes.c_int
+_lib.lora_kv_attend.argtypes = [_P, ctypes.c_int32, _KVS, ctypes.c_float, _P, ctypes.c_int64, _P, ctypes.c_int64, _P]
+_lib.lora_kv_read.restype = ctypes.c_int
+_lib.lora_kv_read.argtypes = [_P, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P, _P]
+_lib.lora_kv_poll_flags.restype = ctypes.c_int
+_lib.lora_kv_poll_flags.argtypes = [_P, ctypes.POINTER(ctypes.c_uint32), _P]
+
+
+def _kv_check(st: int, where: str) -> None:
+    if st != LORA_OK:
+        raise LoraError(st, where)
+
+
+def make_kv_config(n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, n_blocks: int, max_seqs: int,
+                   max_seq_tokens: int, max_tokens: int, slab_ptr: int = 0, slab_bytes: int = 0) -> lora_kv_config:
+    return lora_kv_config(int(n_layers), int(n_heads), int(n_kv_heads), int(head_dim), int(n_blocks), int(max_seqs),
+                          int(max_seq_tokens), int(max_tokens), _P(slab_ptr or None), int(slab_bytes))
+
+
+def lora_kv_slab_bytes(cfg: lora_kv_config) -> int:
+    return int(_lib.lora_kv_slab_bytes(ctypes.byref(cfg)))
+
+
+def lora_kv_create(cfg: lora_kv_config) -> int:
+    """Returns the cache's handle (an integer address); raises LoraError."""
+    h = _P()
+    _kv_check(_lib.lora_kv_create(ctypes.byref(cfg), ctypes.byref(h)), "lora_kv_create")
+    return h.value
+
+
+def lora_kv_destroy(kv: int) -> None:
+    _kv_check(_lib.lora_kv_destroy(_P(kv)), "lora_kv_destroy")
+
+
+def lora_kv_extend(kv: int, n: int, d_seq: int, d_len: int, d_new: int, T: int, max_new: int, stream: int = 0) -> lora_kv_step:
+    step = lora_kv_step()
+    _kv_check(_lib.lora_kv_extend(_P(kv), int(n), _P(d_seq or None), _P(d_len or None), _P(d_new or None), int(T),
+                                  int(max_new), ctypes.byref(step), _P(stream or None)), "lora_kv_extend")
+    return step
+
+
+def lora_kv_release(kv: int, n: int, d_seq: int, d_keep: int = 0, stream: int = 0) -> None:
+    _kv_check(_lib.lora_kv_release(_P(kv), int(n), _P(d_seq or None), _P(d_keep or None), _P(stream or None)), "lora_kv_release")
+
+
+def lora_head_norm_rotate(T: int, n_heads: int, n_kv_heads: int, head_dim: int, d_position: int, heads: lora_heads,
+                          stream: int = 0) -> None:
+    _kv_check(_lib.lora_head_norm_rotate(int(T), int(n_heads), int(n_kv_heads), int(head_dim), _P(d_position or None),
+                                         ctypes.byref(heads), _P(stream or None)), "lora_head_norm_rotate")
+
+
+def lora_kv_store(kv: int, layer: int, step: lora_kv_step, heads: lora_heads, stream: int = 0) -> None:
+    _kv_check(_lib.lora_kv_store(_P(kv), int(layer), ctypes.byref(step), ctypes.byref(heads), _P(stream or None)), "lora_kv_store")
+
+
+def lora_kv_attend(kv: int, layer: int, step: lora_kv_step, scale: float, d_q: int, d_out: int, q_stride: int = 0,
+                   out_stride: int = 0, stream: int = 0) -> None:
+    _kv_check(_lib.lora_kv_attend(_P(kv), int(layer), ctypes.byref(step), float(scale), _P(d_q or None), int(q_stride),
+                                  _P(d_out or None), int(out_stride), _P(stream or None)), "lora_kv_attend")
+
+
+def lora_kv_read(kv: int, layer: int, n: int, d_seq: int, d_position: int, d_k_out: int, d_v_out: int, stream: int = 0) -> None:
+    _kv_check(_lib.lora_kv_read(_P(kv), int(layer), int(n), _P(d_seq or None), _P(d_position or None), _P(d_k_out or None),
+                                _P(d_v_out or None), _P(stream or None)), "lora_kv_read")
+
+
+def lora_kv_poll_flags(kv: int, stream: int = 0) -> Tuple[int, int]:
+    """Returns (status, raw flag word); status is LORA_OK or what the lowest flag stands for."""
+    w = ctypes.c_uint32(0)
+    st = _lib.lora_kv_poll_flags(_P(kv), ctypes.byref(w), _P(stream or None))
+    if st not in (LORA_OK, LORA_ERR_KV_REFUSED, LORA_ERR_KV_EXHAUSTED, LORA_ERR_NOT_FINITE):
+        raise LoraError(st, "lora_kv_poll_flags")
+    return st, int(w.value)

@@ -1,0 +1,270 @@
+// Norm of queries and keys for each head with the position rotation in the same pass, on its own and on the way into the cache in
+// four bits; and the way out of the cache.
+//
+//   u = x / sqrt(mean(x^2) + eps) * w            (where there is a weight)
+//   y_p = u_p cos a - u_p' sin a,  y_p' = u_p' cos a + u_p sin a,   a = position * f_p,  p' = p + D/2 (or its neighbour)
+//
+// One read and one write of every head, so the copy rate bounds it.  D / 8 lanes share a head's row, 16 bytes each; the other half of
+// a rotated pair sits D / 16 lanes away.  Angles are taken in 64 bits (a far position times a frequency has few bits left behind the
+// point in 32) once per token and pair, and shared by all heads through LDS.  Keys on the way to four bits are computed in 64 bits
+// throughout and rounded to 32 once: next to a border between two codes an error of 2^-24 would pick the wrong one now and then.
+#include "kv_device.hpp"
+
+namespace lora {
+namespace kv {
+namespace {
+
+// sin and cos of a in 64 bits: a - n pi/2 with pi/2 in two parts, then the Taylor sums up to r^17 (|r| <= pi/4: the next term is
+// below 2^-56).
+__device__ inline void sin_cos(double a, double& s, double& c)
+{
+    const double n = __builtin_rint(a * 0.63661977236758134308);
+    double r = __builtin_fma(-n, 1.5707963267948966192, a);
+    r = __builtin_fma(-n, 6.1232339957367658e-17, r);
+    const double z = r * r;
+    double ps = 1.0 / 355687428096000.0;
+    ps = __builtin_fma(ps, z, -1.0 / 1307674368000.0);
+    ps = __builtin_fma(ps, z, 1.0 / 6227020800.0);
+    ps = __builtin_fma(ps, z, -1.0 / 39916800.0);
+    ps = __builtin_fma(ps, z, 1.0 / 362880.0);
+    ps = __builtin_fma(ps, z, -1.0 / 5040.0);
+    ps = __builtin_fma(ps, z, 1.0 / 120.0);
+    ps = __builtin_fma(ps, z, -1.0 / 6.0);
+    const double sr = __builtin_fma(ps * z, r, r);
+    double pc = 1.0 / 20922789888000.0;
+    pc = __builtin_fma(pc, z, -1.0 / 87178291200.0);
+    pc = __builtin_fma(pc, z, 1.0 / 479001600.0);
+    pc = __builtin_fma(pc, z, -1.0 / 3628800.0);
+    pc = __builtin_fma(pc, z, 1.0 / 40320.0);
+    pc = __builtin_fma(pc, z, -1.0 / 720.0);
+    pc = __builtin_fma(pc, z, 1.0 / 24.0);
+    pc = __builtin_fma(pc, z, -0.5);
+    const double cr = __builtin_fma(pc, z, 1.0);
+    // quarter turns: n modulo 4 (n itself may not fit an int)
+    const int k = (int)(n - 4.0 * __builtin_floor(n * 0.25));
+    s = (k & 1) ? cr : sr;
+    c = (k & 1) ? sr : cr;
+    if (k == 2 || k == 3) s = -s;
+    if (k == 1 || k == 2) c = -c;
+}
+
+
+// One row of D values: R = float (queries) or double (keys).
+template <int D, typename R>
+__device__ inline void norm_rotate(const u32x4 raw, const uint16_t* weight, float eps, const double2* cs, bool rotate, bool pairs, R (&y)[8])
+{
+    constexpr int L = D / 8;
+    const int l = threadIdx.x % L;
+    R x[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = (R)lo_f32(raw[j]);
+        x[2 * j + 1] = (R)hi_f32(raw[j]);
+    }
+    if (weight) {
+        R sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) sum += __shfl_xor(sum, d);
+        const R mean = sum / (R)D + (R)eps;
+        R inv;
+        if constexpr (sizeof(R) == 8) inv = 1.0 / __builtin_sqrt(mean);
+        else inv = 1.0f / __builtin_sqrtf(mean);
+        const u32x4 w = load16(weight + 8 * l);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] *= inv * (R)lo_f32(w[j]);
+            x[2 * j + 1] *= inv * (R)hi_f32(w[j]);
+        }
+    }
+    if (!rotate) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = x[j];
+    } else if (pairs) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double2 t = cs[4 * l + j];
+            y[2 * j] = x[2 * j] * (R)t.x - x[2 * j + 1] * (R)t.y;
+            y[2 * j + 1] = x[2 * j + 1] * (R)t.x + x[2 * j] * (R)t.y;
+        }
+    } else {
+        const bool second = l >= L / 2;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const R o = __shfl_xor(x[j], L / 2);
+            const double2 t = cs[(8 * l + j) % (D / 2)];
+            y[j] = x[j] * (R)t.x + (second ? o : -o) * (R)t.y;
+        }
+    }
+}
+
+// Eight fp32 values of a lane into codes, their group's exponent shared by four lanes.
+__device__ inline uint32_t to_codes(float (&v)[8], int& exponent, bool& odd)
+{
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (!(__builtin_fabsf(v[j]) <= 3.4028235e38f)) odd = true;
+        if (v[j] != v[j]) v[j] = 0.f;
+        top = fmaxf(top, __builtin_fabsf(v[j]));
+    }
+    top = fmaxf(top, __shfl_xor(top, 1));
+    top = fmaxf(top, __shfl_xor(top, 2));
+    exponent = group_exponent(top);
+    return eight_codes(v, __builtin_bit_cast(float, (uint32_t)exponent << 23));
+}
+
+template <int D> __device__ inline void put_v(uint8_t* part, int k, int l, uint32_t codes)
+{
+    uint8_t* v = part + Part<D>::kV;
+    if constexpr (D == 128) {
+        *reinterpret_cast<uint32_t*>(v + Part<D>::v_at(k, 8 * l)) = codes;
+    } else {
+        *reinterpret_cast<uint16_t*>(v + Part<D>::v_at(k, 8 * l)) = (uint16_t)codes;
+        *reinterpret_cast<uint16_t*>(v + Part<D>::v_at(k, 8 * l + 4)) = (uint16_t)(codes >> 16);
+    }
+}
+template <int D> __device__ inline uint32_t get_v(const uint8_t* part, int k, int l)
+{
+    const uint8_t* v = part + Part<D>::kV;
+    if constexpr (D == 128) return *reinterpret_cast<const uint32_t*>(v + Part<D>::v_at(k, 8 * l));
+    return *reinterpret_cast<const uint16_t*>(v + Part<D>::v_at(k, 8 * l)) |
+           (uint32_t)*reinterpret_cast<const uint16_t*>(v + Part<D>::v_at(k, 8 * l + 4)) << 16;
+}
+
+template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
+{
+    constexpr int L = D / 8, ROWS = 256 / L, P = D / 2;
+    __shared__ double2 cs[TPW][P];
+    const int t0 = blockIdx.x * TPW;
+    const int T = a.cache ? min(a.T, a.head->rows) : a.T;
+    if (t0 >= T) return;
+    const int count = min(TPW, T - t0);
+    const bool rotate = a.inv_freq != nullptr;
+    if (rotate) {
+        for (int k = threadIdx.x; k < count * P; k += 256) {
+            double s, c;
+            sin_cos((double)a.position[t0 + k / P] * (double)a.inv_freq[k % P], s, c);
+            cs[k / P][k % P] = double2{c, s};
+        }
+        __syncthreads();
+    }
+    const int l = threadIdx.x % L;
+    const int nq = a.q ? a.n_heads : 0, nk = a.k ? a.n_kv : 0, nv = a.v ? a.n_kv : 0;
+    const int per = nq + nk + nv;
+    bool odd = false;
+    for (int r = threadIdx.x / L; r < count * per; r += ROWS) {
+        const int tt = r / per, h = r - tt * per;
+        const size_t t = t0 + tt;
+        if (h < nq) {
+            const bool kept = !a.slot || a.slot[t] >= 0;
+            float y[8];
+            norm_rotate<D, float>(load16(a.q + t * a.q_stride + (size_t)h * D + 8 * l), a.q_norm, a.eps, cs[tt], rotate, a.pairs, y);
+            u32x4 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = kept ? pack_bf16(y[2 * j], y[2 * j + 1]) : 0u;
+            *reinterpret_cast<u32x4*>(a.q_out + t * a.q_out_stride + (size_t)h * D + 8 * l) = o;
+            continue;
+        }
+        const bool is_k = h < nq + nk;
+        const int hk = is_k ? h - nq : h - nq - nk;
+        if (is_k && !a.cache) {
+            float y[8];
+            norm_rotate<D, float>(load16(a.k + t * a.k_stride + (size_t)hk * D + 8 * l), a.k_norm, a.eps, cs[tt], rotate, a.pairs, y);
+            u32x4 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = pack_bf16(y[2 * j], y[2 * j + 1]);
+            *reinterpret_cast<u32x4*>(a.k_out + t * a.k_out_stride + (size_t)hk * D + 8 * l) = o;
+            continue;
+        }
+        // into the cache (all lanes of a row agree on what follows)
+        const int slot = a.slot[t];
+        float v[8];
+        if (is_k) {
+            double y[8];
+            norm_rotate<D, double>(load16(a.k + t * a.k_stride + (size_t)hk * D + 8 * l), a.k_norm, a.eps, cs[tt], rotate, a.pairs, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (float)y[j];
+        } else {
+            const u32x4 raw = load16(a.v + t * a.v_stride + (size_t)hk * D + 8 * l);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = lo_f32(raw[j]);
+                v[2 * j + 1] = hi_f32(raw[j]);
+            }
+        }
+        int exponent;
+        bool bad = false;
+        const uint32_t codes = to_codes(v, exponent, bad);
+        if (slot < 0) continue;
+        odd |= bad;
+        uint8_t* part = a.cache + ((size_t)(slot / kBlock) * a.n_kv + hk) * Part<D>::kBytes;
+        const int k = slot % kBlock;
+        if (is_k) *reinterpret_cast<uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l) = codes;
+        else put_v<D>(part, k, l, codes);
+        if (l % 4 == 0)
+            part[is_k ? Part<D>::kKExp + Part<D>::k_exp_at(k, l / 4) : Part<D>::kVExp + Part<D>::v_exp_at(k, l / 4)] = (uint8_t)exponent;
+    }
+    if (odd) atomicOr(&a.head->flags, kFlagNotFinite);
+}
+
+template <int D> __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
+{
+    constexpr int L = D / 8, ROWS = 256 / L;
+    const int l = threadIdx.x % L;
+    const long r = (long)blockIdx.x * ROWS + threadIdx.x / L;
+    const int per = 2 * a.n_kv;
+    if (r >= (long)a.n * per) return;
+    const int t = (int)(r / per), h = (int)(r - (long)t * per);
+    const bool is_v = h >= a.n_kv;
+    const int hk = is_v ? h - a.n_kv : h;
+    const int row = a.seq[t], position = a.position[t];
+    int block = -1;
+    if ((unsigned)row < (unsigned)a.t.max_seqs && position >= 0 && position / kBlock < a.t.held[row])
+        block = a.t.table[(size_t)row * a.t.row_blocks + position / kBlock];
+    u32x4 o = {0, 0, 0, 0};
+    if ((unsigned)block < (unsigned)a.t.n_blocks) {
+        const uint8_t* part = a.cache + ((size_t)block * a.n_kv + hk) * Part<D>::kBytes;
+        const int k = position % kBlock, g = l / 4;
+        const uint32_t codes = is_v ? get_v<D>(part, k, l) : *reinterpret_cast<const uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l);
+        const uint32_t e = part[is_v ? Part<D>::kVExp + Part<D>::v_exp_at(k, g) : Part<D>::kKExp + Part<D>::k_exp_at(k, g)];
+        o = eight_bf16(codes, e << 23);
+    } else if (h == 0 && l == 0) {
+        atomicOr(&a.t.head->flags, kFlagRefused);
+    }
+    uint16_t* out = is_v ? a.v_out : a.k_out;
+    if (out) *reinterpret_cast<u32x4*>(out + (size_t)t * a.n_kv * D + (size_t)hk * D + 8 * l) = o;
+}
+
+template <int D> hipError_t heads(const HeadsArgs& a, hipStream_t stream)
+{
+    // a token of its own per workgroup while that fills no more than the chip; then four, whose angles keep all threads busy
+    if (a.T <= 1024) heads_kernel<D, 1><<<a.T, 256, 0, stream>>>(a);
+    else heads_kernel<D, 4><<<(a.T + 3) / 4, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+template <int D> hipError_t read(const ReadArgs& a, hipStream_t stream)
+{
+    constexpr int rows = 256 / (D / 8);
+    const long n = (long)a.n * 2 * a.n_kv;
+    read_kernel<D><<<(unsigned)((n + rows - 1) / rows), 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_heads(const HeadsArgs& a, int dim, hipStream_t stream)
+{
+    if (a.T == 0) return hipSuccess;
+    return dim == 64 ? heads<64>(a, stream) : heads<128>(a, stream);
+}
+
+hipError_t launch_read(const ReadArgs& a, int dim, hipStream_t stream)
+{
+    if (a.n == 0) return hipSuccess;
+    return dim == 64 ? read<64>(a, stream) : read<128>(a, stream);
+}
+
+}  // namespace kv
+}  // namespace lora

@@ -1,0 +1,278 @@
+// Block tables and slot maps of a step from its requests' lengths, and the list of pieces that its attention is cut into.
+//
+// Request i has l_i tokens in the cache and n_i new ones; it holds h_i blocks of 64 tokens, needs w_i = ceil((l_i + n_i) / 64), and
+// takes max(0, w_i - h_i) blocks more: the lowest free ones, request after request.  A free block is a zero bit of `used`; the k-th
+// free one is found by counting.  Everything is a prefix sum over requests or over bitmap words, integer and so the same whatever
+// order the lanes run in.
+#include "kv_internal.hpp"
+
+#include <algorithm>
+
+namespace lora {
+namespace kv {
+namespace {
+
+constexpr int kWaves = kPlanThreads / 64;
+
+// Exclusive sum over the workgroup's threads of N values each; total[] receives the sums.  sums: [kWaves][N] in LDS.
+template <int N>
+__device__ inline void scan(int (&v)[N], int (&total)[N], int (*sums)[N])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int own[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) own[k] = v[k];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int o = __shfl_up(v[k], d);
+            if (lane >= d) v[k] += o;
+        }
+    __syncthreads();                       // the sums of the scan before have been read
+    if (lane == 63)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sums[wave][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        int before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const int s = sums[w][k];
+            if (w < wave) before += s;
+            all += s;
+        }
+        total[k] = all;
+        v[k] += before - own[k];
+    }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
+{
+    __shared__ int claim[kMaxSeqs];
+    __shared__ int sums[kWaves][4];
+    __shared__ unsigned long long work;
+    const int tid = threadIdx.x;
+    const Tables& t = a.t;
+    const int n = a.n, T = a.T;
+    uint32_t flags = 0;
+
+    // a row named twice belongs to the first request that names it
+    for (int r = tid; r < t.max_seqs; r += kPlanThreads) claim[r] = n;
+    if (tid == 0) work = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kPlanThreads) {
+        const int row = a.seq[i];
+        if ((unsigned)row < (unsigned)t.max_seqs) atomicMin(&claim[row], i);
+    }
+    __syncthreads();
+
+    // token rows and blocks of every request
+    int rows0 = 0, need0 = 0;
+    for (int base = 0; base < n; base += kPlanThreads) {
+        const int i = base + tid;
+        Request q = {};
+        bool ok = false;
+        int add = 0;
+        if (i < n) {
+            q.row = a.seq[i];
+            q.len = a.len[i];
+            add = a.add[i];
+            const bool own = (unsigned)q.row < (unsigned)t.max_seqs && claim[q.row] == i;
+            q.held = own ? t.held[q.row] : -1;
+            ok = own && q.len >= 0 && add >= 0 && add <= a.max_new && q.len <= t.max_seq_tokens && add <= t.max_seq_tokens - q.len &&
+                 (q.len + kBlock - 1) / kBlock <= q.held;
+        }
+        // the sums stop at T + 1: what lies behind is outside of the step in any case
+        int v[1] = {add < 0 ? 0 : min(add, T + 1)}, total[1];
+        const int mine = v[0];
+        scan<1>(v, total, reinterpret_cast<int(*)[1]>(sums));
+        q.first = min(rows0 + v[0], T + 1);
+        rows0 = min(rows0 + total[0], T + 1);
+        ok = ok && q.first + mine <= T;
+        if (i < n) {
+            q.rows = max(0, min(q.first + mine, T) - q.first);
+            q.first = min(q.first, T);
+            t.start[i] = q.first;
+            q.want = ok ? max(q.held, (q.len + mine + kBlock - 1) / kBlock) : 0;
+            if (!ok) flags |= kFlagRefused;
+        }
+        int w[1] = {ok ? q.want - q.held : 0}, wt[1];
+        scan<1>(w, wt, reinterpret_cast<int(*)[1]>(sums));
+        q.fresh = need0 + w[0];
+        need0 += wt[0];
+        if (i < n) {
+            if (!ok) q.held = -1;
+            t.request[i] = q;
+        }
+    }
+    if (tid == 0) {
+        t.start[n] = min(rows0, T);
+        t.head->rows = min(rows0, T);
+    }
+
+    // the first need0 free blocks in ascending order; 32 of them a bitmap word
+    int found = 0;
+    for (int base = 0; base < t.n_words && found < need0; base += kPlanThreads) {
+        const int w = base + tid;
+        uint32_t free = w < t.n_words ? ~t.used[w] : 0u;
+        if (w == t.n_words - 1 && (t.n_blocks & 31)) free &= (1u << (t.n_blocks & 31)) - 1;
+        int v[1] = {(int)__popc(free)}, total[1];
+        scan<1>(v, total, reinterpret_cast<int(*)[1]>(sums));
+        int at = found + v[0];
+        while (free && at < need0) {
+            const int b = __ffs(free) - 1;
+            free &= free - 1;
+            t.fresh[at++] = w * 32 + b;
+        }
+        found += total[0];
+    }
+    found = min(found, need0);
+
+    // who gets them; how much attention has to read
+    int taken = 0;
+    unsigned long long mine = 0;
+    for (int i = tid; i < n; i += kPlanThreads) {
+        Request q = t.request[i];
+        q.tiles = (q.rows * a.group + kFewCols - 1) / kFewCols;
+        if (q.held >= 0) {
+            if (q.want > q.held && q.fresh + (q.want - q.held) > found) {
+                flags |= kFlagExhausted;
+                q.held = -1;
+            } else {
+                taken = max(taken, q.want > q.held ? q.fresh + (q.want - q.held) : 0);
+                mine += (unsigned long long)q.tiles * (unsigned)((q.len + q.rows + kBlock - 1) / kBlock);
+            }
+        }
+        t.request[i] = q;
+    }
+    if (mine) atomicAdd(&work, mine);
+    for (int d = 32; d; d >>= 1) taken = max(taken, __shfl_xor(taken, d));
+    __syncthreads();
+    if ((tid & 63) == 0) sums[tid >> 6][0] = taken;
+    __syncthreads();
+    taken = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) taken = max(taken, sums[w][0]);
+    for (int k = tid; k < taken; k += kPlanThreads) {
+        const int b = t.fresh[k];
+        atomicOr(&t.used[b >> 5], 1u << (b & 31));
+    }
+
+    // pieces of attention: every tile's keys are cut so that all tiles and key heads together make kFewItems pieces, and at most one more
+    // per tile; the four waves of a workgroup take a piece's blocks in turn
+    const unsigned long long per = (work * a.n_kv + kFewItems - 1) / kFewItems;
+    const int chunk = ((int)(per < 4 ? 4 : per > kMaxBlocks ? kMaxBlocks : per) + 3) & ~3;
+    int e0 = 0, p0 = 0, m0 = 0;
+    for (int base = 0; base < n; base += kPlanThreads) {
+        const int i = base + tid;
+        Request q = {};
+        int v[3] = {0, 0, 0}, total[3];
+        if (i < n) {
+            q = t.request[i];
+            const int blocks = q.held >= 0 ? (q.len + q.rows + kBlock - 1) / kBlock : 0;
+            q.splits = max(1, (blocks + chunk - 1) / chunk);
+            q.chunk = (blocks + q.splits - 1) / q.splits;
+            v[0] = q.tiles * q.splits;
+            v[1] = q.splits > 1 ? q.tiles * q.splits : 0;
+            v[2] = q.splits > 1 ? q.tiles : 0;
+        }
+        scan<3>(v, total, reinterpret_cast<int(*)[3]>(sums));
+        if (i < n) {
+            q.entry = e0 + v[0];
+            q.part = p0 + v[1];
+            q.merge = m0 + v[2];
+            t.request[i] = q;
+        }
+        e0 += total[0];
+        p0 += total[1];
+        m0 += total[2];
+    }
+    if (tid == 0) {
+        t.head->n_few = e0;
+        t.head->n_merge = m0;
+    }
+    if (flags) atomicOr(&t.head->flags, flags);
+}
+
+// What plan_kernel has decided, written out: a workgroup per request and kFillRows of its token rows.
+constexpr int kFillRows = 1024;
+__global__ __launch_bounds__(256) void fill_kernel(PlanArgs a)
+{
+    const Tables& t = a.t;
+    const Request q = t.request[blockIdx.x];
+    int32_t* row = t.table + (size_t)(q.held >= 0 ? q.row : 0) * t.row_blocks;
+    // (a refused request may have more rows than max_new, for which the grid was made)
+    for (int j = blockIdx.y * 256 + (int)threadIdx.x; j < q.rows; j += gridDim.y * 256) {
+        int position = -1, slot = -1;
+        if (q.held >= 0) {
+            position = q.len + j;
+            const int b = position / kBlock;
+            slot = (b < q.held ? row[b] : t.fresh[q.fresh + b - q.held]) * kBlock + position % kBlock;
+        }
+        t.position[q.first + j] = position;
+        t.slot[q.first + j] = slot;
+    }
+    if (blockIdx.y) return;
+    if (q.held >= 0) {
+        for (int b = q.held + (int)threadIdx.x; b < q.want; b += 256) row[b] = t.fresh[q.fresh + b - q.held];
+        if (threadIdx.x == 0) t.held[q.row] = q.want;
+    }
+    for (int k = threadIdx.x; k < q.tiles * q.splits; k += 256) {
+        Entry e = {};
+        e.request = blockIdx.x;
+        e.tile = k / q.splits;
+        e.block = (k % q.splits) * q.chunk;
+        // the last token of the tile sees this many blocks
+        const int last = min(q.rows - 1, ((e.tile + 1) * kFewCols - 1) / a.group);
+        const int seen = q.held >= 0 ? (q.len + last) / kBlock + 1 : 0;
+        e.blocks = max(0, min(q.chunk, seen - e.block));
+        e.part = q.splits > 1 ? q.part + k : -1;
+        t.few[q.entry + k] = e;
+    }
+    if (q.splits > 1)
+        for (int k = threadIdx.x; k < q.tiles; k += 256) t.merge[q.merge + k] = Merge{(int)blockIdx.x, k, q.part + k * q.splits, q.splits};
+}
+
+__global__ __launch_bounds__(64) void release_kernel(Tables t, const int32_t* seq, const int32_t* keep)
+{
+    const int i = blockIdx.x;
+    const int row = seq[i], tokens = keep ? keep[i] : 0;
+    if ((unsigned)row >= (unsigned)t.max_seqs || tokens < 0) {
+        if (threadIdx.x == 0) atomicOr(&t.head->flags, kFlagRefused);
+        return;
+    }
+    const int k = (int)(((long)tokens + kBlock - 1) / kBlock);
+    int held = 0;
+    // a row named twice: whoever lowers the count gives back what lies in between
+    if (threadIdx.x == 0) held = atomicMin(&t.held[row], k);
+    held = __shfl(held, 0);
+    int32_t* blocks = t.table + (size_t)row * t.row_blocks;
+    for (int b = k + (int)threadIdx.x; b < held; b += 64) {
+        const int blk = blocks[b];
+        blocks[b] = -1;
+        atomicAnd(&t.used[blk >> 5], ~(1u << (blk & 31)));
+    }
+}
+
+}  // namespace
+
+hipError_t launch_plan(const PlanArgs& a, hipStream_t stream)
+{
+    plan_kernel<<<1, kPlanThreads, 0, stream>>>(a);
+    if (a.n > 0) {
+        const int chunks = std::max(1, (a.max_new + kFillRows - 1) / kFillRows);
+        fill_kernel<<<dim3(a.n, chunks), 256, 0, stream>>>(a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_release(const Tables& t, int n, const int32_t* seq, const int32_t* keep, hipStream_t stream)
+{
+    if (n > 0) release_kernel<<<n, 64, 0, stream>>>(t, seq, keep);
+    return hipGetLastError();
+}
+
+}  // namespace kv
+}  // namespace lora

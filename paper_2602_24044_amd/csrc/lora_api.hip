@@ -34,6 +34,14 @@ inline bool hip_fail(hipError_t e, const char* what)
 }
 #define HIP_FAIL(call) hip_fail((call), #call)
 
+}  // namespace
+
+namespace lora {
+bool note_hip_failure(hipError_t e, const char* what) { return hip_fail(e, what); }
+}  // namespace lora
+
+namespace {
+
 // Device address of `scratch` on the current device, looked up once per device (with that device current).
 constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mutex;
@@ -577,6 +585,9 @@ const char* lora_status_string(lora_status status)
         case LORA_ERR_ID_RANGE: return "adapter id out of range";
         case LORA_ERR_STARVATION: return "no starvation-free placement";
         case LORA_ERR_SCRATCH_LIMIT: return "the call needs more scratch than the library's static buffer holds";
+        case LORA_ERR_KV_REFUSED: return "a request or token of the cache was refused";
+        case LORA_ERR_KV_EXHAUSTED: return "no free block in the cache";
+        case LORA_ERR_NOT_FINITE: return "a key or value was not finite";
     }
     return "unknown status";
 }

@@ -317,3 +317,193 @@ class ModelSession:
             self.close()
         except Exception:
             pass
+
+
+# ---- key/value cache in four bits ----
+def _stream_of(stream: Optional[torch.cuda.Stream]) -> int:
+    return (stream or torch.cuda.current_stream()).cuda_stream
+
+
+def _rows(t: torch.Tensor, width: int, rows: int, device, what: str) -> int:
+    """Stride in elements between the rows of a bf16 operand [rows, width] whose rows are contiguous; raises ValueError."""
+    if t.dtype != torch.bfloat16 or t.device != device or t.dim() != 2 or t.shape != (rows, width):
+        raise ValueError(f"{what}: bf16 [{rows}, {width}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.stride(1) != 1 or (rows > 1 and t.stride(0) < width):
+        raise ValueError(f"{what}: the values of a row must lie next to each other, and rows must not overlap")
+    return t.stride(0) if rows > 1 else width
+
+
+def _ints(t: torch.Tensor, n: Optional[int], device, what: str) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 [{'n' if n is None else n}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+def _heads(dim: int, device, inv_freq, q_norm, k_norm, eps: float, pairing: int) -> B.lora_heads:
+    h = B.lora_heads()
+    if inv_freq is not None:
+        if inv_freq.dtype != torch.float32 or inv_freq.device != device or inv_freq.shape != (dim // 2,) or not inv_freq.is_contiguous():
+            raise ValueError(f"inv_freq: contiguous float32 [{dim // 2}] on {device} expected")
+        h.d_inv_freq = inv_freq.data_ptr()
+    for w, name in ((q_norm, "d_q_norm"), (k_norm, "d_k_norm")):
+        if w is not None:
+            if w.dtype != torch.bfloat16 or w.device != device or w.shape != (dim,) or not w.is_contiguous():
+                raise ValueError(f"{name[2:]}: contiguous bfloat16 [{dim}] on {device} expected")
+            setattr(h, name, w.data_ptr())
+    h.eps = float(eps)
+    h.pairing = int(pairing)
+    return h
+
+
+def rotary_inv_freq(head_dim: int, base: float, device) -> torch.Tensor:
+    """base^(-2 p / head_dim) for the pairs p of a head, as the rotation takes it (fp32)."""
+    p = torch.arange(0, head_dim, 2, dtype=torch.float64)
+    return (1.0 / base ** (p / head_dim)).to(torch.float32).to(device)
+
+
+def head_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], n_heads: int, n_kv_heads: int,
+                     position: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor] = None,
+                     q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     pairing: int = B.LORA_ROTATE_HALVES, q_out: Optional[torch.Tensor] = None,
+                     k_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Norm and rotation of q [T, n_heads * dim] and k [T, n_kv_heads * dim] (lora_head_norm_rotate); returns the outputs."""
+    some = q if q is not None else k
+    if some is None or some.dim() != 2:
+        raise ValueError("q or k: bf16 [T, heads * dim] expected")
+    T, device = some.shape[0], some.device
+    dim = some.shape[1] // max(n_heads if q is not None else n_kv_heads, 1)
+    h = _heads(dim, device, inv_freq, q_norm, k_norm, eps, pairing)
+    with torch.cuda.device(device):
+        if q is not None:
+            q_out = torch.empty((T, n_heads * dim), dtype=torch.bfloat16, device=device) if q_out is None else q_out
+            h.d_q, h.q_stride = q.data_ptr(), _rows(q, n_heads * dim, T, device, "q")
+            h.d_q_out, h.q_out_stride = q_out.data_ptr(), _rows(q_out, n_heads * dim, T, device, "q_out")
+        if k is not None:
+            k_out = torch.empty((T, n_kv_heads * dim), dtype=torch.bfloat16, device=device) if k_out is None else k_out
+            h.d_k, h.k_stride = k.data_ptr(), _rows(k, n_kv_heads * dim, T, device, "k")
+            h.d_k_out, h.k_out_stride = k_out.data_ptr(), _rows(k_out, n_kv_heads * dim, T, device, "k_out")
+        if T:
+            d_pos = 0 if position is None else _ints(position, T, device, "position").data_ptr()
+            B.lora_head_norm_rotate(T, n_heads, n_kv_heads, dim, d_pos, h, _stream_of(stream))
+    return q_out, k_out
+
+
+class KvStep:
+    """The step of the latest KvCache.extend: its arrays as tensors on the cache's memory."""
+
+    def __init__(self, kv: "KvCache", raw: B.lora_kv_step):
+        self.raw = raw
+        self.n, self.T = int(raw.n), int(raw.T)
+        self.start = kv._view(raw.start, self.n + 1)
+        self.position = kv._view(raw.position, self.T)
+        self.slot = kv._view(raw.slot, self.T)
+        self.table = kv._view(raw.table, kv.max_seqs * int(raw.row_blocks)).view(kv.max_seqs, int(raw.row_blocks))
+        self.held = kv._view(raw.held, kv.max_seqs)
+
+
+class KvCache:
+    """Keys and values of the running sequences in four bits, for every decoder layer (lora_kv_*): owns the device memory
+    and forwards to the C ABI.  No arithmetic of the method happens here."""
+
+    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, n_blocks: int, max_seqs: int,
+                 max_seq_tokens: int, max_tokens: int, device: str = "cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("liblora_mi355 needs a GPU; there is no CPU path")
+        self.kv = 0
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
+        self.n_blocks, self.max_seqs = n_blocks, max_seqs
+        cfg = B.make_kv_config(n_layers, n_heads, n_kv_heads, head_dim, n_blocks, max_seqs, max_seq_tokens, max_tokens)
+        self.nbytes = B.lora_kv_slab_bytes(cfg)
+        with torch.cuda.device(self.device):
+            if self.nbytes:
+                self.slab = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
+                cfg.slab, cfg.slab_bytes = self.slab.data_ptr(), self.nbytes
+            self.kv = B.lora_kv_create(cfg)       # says what is wrong with a shape that has no slab
+        self.step: Optional[KvStep] = None
+
+    def _view(self, ptr: int, n: int) -> torch.Tensor:
+        off = int(ptr) - self.slab.data_ptr()
+        assert 0 <= off and off + 4 * n <= self.slab.numel()
+        return self.slab[off:off + 4 * n].view(torch.int32)
+
+    def _current_step(self) -> KvStep:
+        if self.step is None:
+            raise ValueError("no step: call extend first")
+        return self.step
+
+    def extend(self, seq: torch.Tensor, length: torch.Tensor, new: torch.Tensor, T: int, max_new: Optional[int] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> KvStep:
+        """Blocks and places for the next `new[i]` tokens of the sequences in rows `seq[i]`, which have `length[i]` tokens."""
+        n = int(seq.shape[0])
+        ptr = [_ints(t, n, self.device, what).data_ptr() if n else 0 for t, what in ((seq, "seq"), (length, "length"), (new, "new"))]
+        with torch.cuda.device(self.device):
+            raw = B.lora_kv_extend(self.kv, n, *ptr, T, T if max_new is None else max_new, _stream_of(stream))
+        self.step = KvStep(self, raw)
+        return self.step
+
+    def release(self, seq: torch.Tensor, keep: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Gives back the blocks of the rows `seq` behind their first `keep[i]` tokens (none are kept without `keep`)."""
+        n = int(seq.shape[0])
+        d_seq = _ints(seq, n, self.device, "seq").data_ptr() if n else 0
+        d_keep = _ints(keep, n, self.device, "keep").data_ptr() if n and keep is not None else 0
+        with torch.cuda.device(self.device):
+            B.lora_kv_release(self.kv, n, d_seq, d_keep, _stream_of(stream))
+        self.step = None
+
+    def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+              inv_freq: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
+              k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, pairing: int = B.LORA_ROTATE_HALVES,
+              out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+        """The step's keys (normed, rotated) and values into the layer's cache; returns the normed and rotated queries."""
+        step = self._current_step()
+        h = _heads(self.head_dim, self.device, inv_freq, q_norm, k_norm, eps, pairing)
+        wq, wk = self.n_heads * self.head_dim, self.n_kv_heads * self.head_dim
+        with torch.cuda.device(self.device):
+            h.d_k, h.k_stride = k.data_ptr(), _rows(k, wk, step.T, self.device, "k")
+            h.d_v, h.v_stride = v.data_ptr(), _rows(v, wk, step.T, self.device, "v")
+            if q is not None:
+                out = torch.empty((step.T, wq), dtype=torch.bfloat16, device=self.device) if out is None else out
+                h.d_q, h.q_stride = q.data_ptr(), _rows(q, wq, step.T, self.device, "q")
+                h.d_q_out, h.q_out_stride = out.data_ptr(), _rows(out, wq, step.T, self.device, "out")
+            B.lora_kv_store(self.kv, layer, step.raw, h, _stream_of(stream))
+        return out
+
+    def attend(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Attention of the step's tokens over the layer's cache; scale: 1 / sqrt(head_dim) unless given."""
+        step = self._current_step()
+        w = self.n_heads * self.head_dim
+        with torch.cuda.device(self.device):
+            out = torch.empty((step.T, w), dtype=torch.bfloat16, device=self.device) if out is None else out
+            B.lora_kv_attend(self.kv, layer, step.raw, self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(),
+                             _rows(q, w, step.T, self.device, "q"), _rows(out, w, step.T, self.device, "out"), _stream_of(stream))
+        return out
+
+    def read(self, layer: int, seq: torch.Tensor, position: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
+        """Keys and values of the tokens (seq[i], position[i]) as the bf16 values that their codes stand for."""
+        n = int(seq.shape[0])
+        with torch.cuda.device(self.device):
+            k, v = (torch.empty((n, self.n_kv_heads * self.head_dim), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            if n:
+                B.lora_kv_read(self.kv, layer, n, _ints(seq, n, self.device, "seq").data_ptr(),
+                               _ints(position, n, self.device, "position").data_ptr(), k.data_ptr(), v.data_ptr(), _stream_of(stream))
+        return k, v
+
+    def poll(self, stream: Optional[torch.cuda.Stream] = None):
+        """(status, flag word) since the last poll."""
+        with torch.cuda.device(self.device):
+            return B.lora_kv_poll_flags(self.kv, _stream_of(stream))
+
+    def close(self):
+        if self.kv:
+            B.lora_kv_destroy(self.kv)
+            self.kv = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
