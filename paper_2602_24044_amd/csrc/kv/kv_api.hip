@@ -41,9 +41,13 @@ lora_status check_config(const lora_kv_config* c)
 struct Layout {
     size_t layer_bytes = 0;
     size_t cache = 0, table = 0, held = 0, used = 0, head = 0, fresh = 0, start = 0, position = 0, slot = 0, request = 0, few = 0,
-           merge = 0, part_acc = 0, part_ml = 0, total = 0;
-    long max_entries = 0;
+           many = 0, merge = 0, few_acc = 0, few_ml = 0, many_acc = 0, many_ml = 0, total = 0;
 };
+
+// Entries that the lists of a step of T tokens in n requests can have: one a tile, and at most kFewItems (kManyItems) more, counted
+// with the key heads, where tiles are cut along their keys.
+long most_few(long n, int n_kv) { return n * (kFewMost / kFewCols) + kFewItems / n_kv + 1; }
+long most_many(long T, long n, int group, int n_kv) { return T * group / kManyCols + std::min(n, T * group / kFewMost) + kManyItems / n_kv + 1; }
 
 Layout make_layout(const lora_kv_config* c)
 {
@@ -62,15 +66,22 @@ Layout make_layout(const lora_kv_config* c)
     L.position = take(4 * T);
     L.slot = take(4 * T);
     L.request = take(sizeof(Request) * seqs);
-    // one entry a tile, and at most kFewItems more, counted with the key heads, where tiles are cut along their keys; every cut
-    // tile has a partial result per piece, and a cut piece is at least half of what a cut is aimed at
-    const size_t tiles = T * group / kFewCols + seqs;
-    L.max_entries = (long)(tiles + kFewItems / c->n_kv_heads + 1);
-    L.few = take(sizeof(Entry) * (size_t)L.max_entries);
-    L.merge = take(sizeof(Merge) * (tiles + 1));
-    const size_t parts = (2 * (size_t)kFewItems / c->n_kv_heads + 2) * c->n_kv_heads;
-    L.part_acc = take(4 * parts * kFewCols * (size_t)c->head_dim);
-    L.part_ml = take(4 * parts * kFewCols * 2);
+    const int n_kv = c->n_kv_heads;
+    const size_t few = (size_t)most_few(seqs, n_kv), many = (size_t)most_many(T, seqs, (int)group, n_kv);
+    L.few = take(sizeof(Entry) * few);
+    L.many = take(sizeof(Entry) * many);
+    L.merge = take(sizeof(Merge) * (few + many));
+    // a cut tile has a partial result per piece, and its pieces are at least half of what a cut is aimed at; nor are there more than the
+    // smallest pieces make
+    auto parts = [&](size_t items, size_t entries, int least) {
+        const size_t splits = ((size_t)row_blocks_of(c) + least - 1) / least;
+        return std::min((2 * items / n_kv + 2), splits > 1 ? entries * splits : 0) * n_kv;
+    };
+    const size_t pf = parts(kFewItems, few, kFewChunk), pm = T * group > (size_t)kFewMost ? parts(kManyItems, many, kManyChunk) : 0;
+    L.few_acc = take(4 * pf * kFewCols * (size_t)c->head_dim);
+    L.few_ml = take(4 * pf * kFewCols * 2);
+    L.many_acc = take(4 * pm * kManyCols * (size_t)c->head_dim);
+    L.many_ml = take(4 * pm * kManyCols * 2);
     L.total = o;
     return L;
 }
@@ -154,6 +165,7 @@ struct lora_kv {
         t.slot = at<int32_t>(L.slot);
         t.request = at<Request>(L.request);
         t.few = at<Entry>(L.few);
+        t.many = at<Entry>(L.many);
         t.merge = at<Merge>(L.merge);
         t.n_blocks = cfg.n_blocks;
         t.n_words = (cfg.n_blocks + 31) / 32;
@@ -326,13 +338,16 @@ lora_status lora_kv_attend(lora_kv* k, int32_t layer, const lora_kv_step* step, 
     a.out = static_cast<uint16_t*>(d_out);
     a.q_stride = q_stride;
     a.out_stride = out_stride;
-    a.part_acc = k->at<float>(k->L.part_acc);
-    a.part_ml = k->at<float>(k->L.part_ml);
+    a.few_acc = k->at<float>(k->L.few_acc);
+    a.few_ml = k->at<float>(k->L.few_ml);
+    a.many_acc = k->at<float>(k->L.many_acc);
+    a.many_ml = k->at<float>(k->L.many_ml);
     a.scale_log2 = scale * 1.44269504088896340736f;
     a.T = step->T;
     a.n_kv = k->cfg.n_kv_heads;
     a.group = k->cfg.n_heads / k->cfg.n_kv_heads;
-    return KV_HIP_FAIL(launch_attend(a, k->cfg.head_dim, k->n_cus, k->L.max_entries, s)) ? LORA_ERR_HIP : LORA_OK;
+    const long few = most_few(step->n, a.n_kv), many = most_many(step->T, step->n, a.group, a.n_kv);
+    return KV_HIP_FAIL(launch_attend(a, k->cfg.head_dim, k->n_cus, few, (long)step->T * a.group > kFewMost ? many : 0, s)) ? LORA_ERR_HIP : LORA_OK;
 }
 
 lora_status lora_kv_read(lora_kv* k, int32_t layer, int32_t n, const int32_t* d_seq, const int32_t* d_position, void* d_k_out, void* d_v_out,

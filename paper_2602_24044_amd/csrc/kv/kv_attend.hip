@@ -6,8 +6,11 @@
 // grows.  Scores, weights' sums, m and the accumulated values are fp32; the weights are rounded to bf16 for the matrix units (2^-9 of
 // each, like the values' own rounding in a cache of 16 bits).
 //
+// Two kernels share the work.  Of a request with few columns (one-token requests) a wave takes whole blocks and converts what it
+// needs itself: the cache's bytes bound it.  For long chunks four waves share the converted keys and values through LDS.
+//
 // A column is a query: (token j, head g of the key head's group), column j * group + g, so a group's heads share the keys that they
-// read.  S^T = K Q^T and O^T = V^T P^T on 16x16x32 MFMAs, 16 columns a tile: a lane's results belong to one column, the
+// read.  S^T = K Q^T and O^T = V^T P^T on 16x16x32 MFMAs (32x32x16 in the second kernel): a lane's results belong to one column, the
 // accumulator of S^T (lane (c, quarter): keys 4 quarter + i of a 16-key tile) is the operand that the second product wants once its 32
 // keys are counted in that order, and the codes of four keys and eight dimensions that a lane loads with one instruction are
 // its own part of V^T, so neither the weights nor the values cross lanes or LDS.
@@ -143,10 +146,9 @@ template <int D> __device__ inline void one_block(Running<D>& r, const Codes<D>&
     }
 }
 
-// Row of the output and of the queries that column c of a tile is; false: there is none.
-__device__ inline bool column(const Request& r, int group, int T, int tile, int c, int& token, int& head)
+// Token and head that a request's column is; false: there is none in the step.
+__device__ inline bool column(const Request& r, int group, int T, int col, int& token, int& head)
 {
-    const int col = tile * kFewCols + c;
     token = col / group;
     head = col - token * group;
     return token < r.rows && r.first + token < T;
@@ -165,7 +167,7 @@ template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(Attend
         const int h = item % a.n_kv;
         const Request r = a.t.request[e.request];
         int token, head;
-        const bool real = column(r, a.group, a.T, e.tile, c, token, head);
+        const bool real = column(r, a.group, a.T, e.tile * kFewCols + c, token, head);
         const int limit = r.len + token;                                    // last key that the lane's column sees
         Running<D> run;
         run.m = -INFINITY;
@@ -181,8 +183,8 @@ template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(Attend
         }
         const int32_t* blocks = a.t.table + (size_t)(r.held >= 0 ? r.row : 0) * a.t.row_blocks;
         for (int b = e.block + wave; b < e.block + e.blocks; b += 4) {
-            const int at = blocks[b];
-            if ((unsigned)at >= (unsigned)a.t.n_blocks) continue;           // the row has been released since the plan
+            // (a row that has been released since the plan has no block there)
+            const int at = min((unsigned)blocks[b], (unsigned)a.t.n_blocks - 1);
             Codes<D> codes;
             load_block<D>(codes, a.cache + ((size_t)at * a.n_kv + h) * Part<D>::kBytes, lane);
             one_block<D>(run, codes, q, a.scale_log2, limit - b * kBlock, b * kBlock + kBlock - 1 > r.len, quad);
@@ -204,7 +206,7 @@ template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(Attend
         __syncthreads();
         constexpr int V = D * kFewCols / 256;                               // values of a thread
         const int cc = tid / 16, d0 = (tid % 16) * V;
-        if (!column(r, a.group, a.T, e.tile, cc, token, head)) continue;    // (no barrier behind this in the loop but the next item's first)
+        if (!column(r, a.group, a.T, e.tile * kFewCols + cc, token, head)) continue;    // (no barrier behind this in the loop but the next item's first)
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 4; ++w) m = fmaxf(m, sM[w][cc]);
@@ -222,10 +224,10 @@ template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(Attend
         if (e.part >= 0) {
             const size_t slot = ((size_t)e.part * a.n_kv + h) * kFewCols + cc;
 #pragma unroll
-            for (int j = 0; j < V; ++j) a.part_acc[slot * D + d0 + j] = acc[j];
+            for (int j = 0; j < V; ++j) a.few_acc[slot * D + d0 + j] = acc[j];
             if (tid % 16 == 0) {
-                a.part_ml[slot * 2] = m;
-                a.part_ml[slot * 2 + 1] = l;
+                a.few_ml[slot * 2] = m;
+                a.few_ml[slot * 2 + 1] = l;
             }
         } else {
             const float f = l == 0.f ? 0.f : 1.0f / l;                      // no key at all: a refused request, its rows are zero
@@ -236,52 +238,285 @@ template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(Attend
     }
 }
 
-// The partial results of a tile that was cut along its keys.
-template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs a)
+// ---- tiles of many columns ----
+// A workgroup's codes of a block of 64 keys, as its 256 threads load them: K: key tid / 4, a quarter of its dimensions; V: two
+// chunks of four keys (those that a lane of the second product wants together), kE dimensions, of which the thread converts half.
+template <int D> struct Raw {
+    uint32_t k[D / 32], v[2][D / 32], ke, ve[2];
+};
+
+struct Place {
+    int key, quarter;          // K
+    int u, h, half, m;         // V: keys 16 u + 4 h .. + 3 and 16 u + 8 + 4 h .. + 3, dimensions kE m .. 
+};
+__device__ inline Place place()
 {
-    constexpr int V = D * kFewCols / 256;
-    const int tid = threadIdx.x, cc = tid / 16, d0 = (tid % 16) * V;
-    const int n_items = a.t.head->n_merge * a.n_kv;
-    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-        const Merge g = a.t.merge[item / a.n_kv];
-        const int h = item % a.n_kv;
-        const Request r = a.t.request[g.request];
-        int token, head;
-        if (!column(r, a.group, a.T, g.tile, cc, token, head)) continue;
-        float m = -INFINITY;
-        for (int s = 0; s < g.splits; ++s) m = fmaxf(m, a.part_ml[(((size_t)(g.part + s) * a.n_kv + h) * kFewCols + cc) * 2]);
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f, acc[V];
+    const int t = threadIdx.x;
+    return Place{t >> 2, t & 3, t >> 6, (t >> 5) & 1, (t >> 4) & 1, t & 15};
+}
+
+template <int D> __device__ inline void load_raw(Raw<D>& r, const uint8_t* part, const Place& p)
+{
+    using P = Part<D>;
+    load_words(r.k, part + P::kK + p.key * P::kRow + p.quarter * (D / 8));
+    r.ke = part[P::kKExp + P::k_exp_at(p.key, p.quarter * (D / 4) / kGroup)];
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
-        for (int s = 0; s < g.splits; ++s) {
-            const size_t slot = ((size_t)(g.part + s) * a.n_kv + h) * kFewCols + cc;
-            const float f = exp2_fast(a.part_ml[slot * 2] - base);
-            l += f * a.part_ml[slot * 2 + 1];
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += f * a.part_acc[slot * D + d0 + j];
-        }
-        const float f = l == 0.f ? 0.f : 1.0f / l;
-        uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + d0;
-#pragma unroll
-        for (int j = 0; j < V; j += 2) *reinterpret_cast<uint32_t*>(o + j) = pack_bf16(acc[j] * f, acc[j + 1] * f);
+    for (int c = 0; c < 2; ++c) {
+        load_words(r.v[c], part + P::kV + P::v_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE));
+        r.ve[c] = *reinterpret_cast<const uint32_t*>(part + P::kVExp + P::v_exp_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE / kGroup));
     }
 }
 
-template <int D> hipError_t attend(const AttendArgs& a, int n_cus, long max_entries, hipStream_t stream)
+// The block in LDS: every operand of an MFMA is 64 lanes * 16 bytes, in lane order but for a permutation inside groups of eight that
+// spreads a wave's writes over the banks.  K: [key / 32][D / 16], V: [d / 32][key / 16].
+template <int D> struct Tile {
+    static constexpr int kKFrags = 2 * (D / 16), kVFrags = (D / 32) * 4;
+    u32x4 k[kKFrags * 64], v[kVFrags * 64];
+    __device__ static int k_at(int tile, int s, int h, int i) { return (tile * (D / 16) + s) * 64 + h * 32 + (i ^ (2 * (s * 16 / (D / 4)))); }
+    __device__ static int v_at(int dt, int u, int h, int i) { return (dt * 4 + u) * 64 + h * 32 + (i ^ (2 * ((i >> 3) & 3) + (dt & 1))); }
+};
+
+template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, const Place& p)
 {
-    const int grid = (int)std::max<long>(1, std::min<long>(max_entries * a.n_kv, 4L * n_cus));
+    constexpr int E = Part<D>::kE;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        const int d = p.quarter * (D / 4) + 8 * j;
+        t.k[Tile<D>::k_at(p.key >> 5, d >> 4, (d >> 3) & 1, p.key & 31)] = eight_bf16(r.k[j], r.ke << 23);
+    }
+    u32x4 f[E / 2];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {                      // keys 2 x, 2 x + 1 of the thread's eight
+        const int c = x / 2, i = 2 * (x & 1);
+        const uint32_t e0 = i == 0 ? r.ve[c] << 23 : r.ve[c] << 7, e1 = i == 0 ? r.ve[c] << 15 : r.ve[c] >> 1;
+        uint32_t a, b;
+        if constexpr (D == 128) {
+            a = r.v[c][i] >> (16 * p.half);
+            b = r.v[c][i + 1] >> (16 * p.half);
+        } else {
+            a = r.v[c][i / 2] >> (8 * p.half);
+            b = a >> 16;
+        }
+#pragma unroll
+        for (int j = 0; j < E / 4; ++j) {
+            const uint32_t y = j == 0 ? two_bf16<0>(a, e0) : two_bf16<1>(a, e0), z = j == 0 ? two_bf16<0>(b, e1) : two_bf16<1>(b, e1);
+            f[2 * j][x] = __builtin_amdgcn_perm(z, y, 0x05040100u);
+            f[2 * j + 1][x] = __builtin_amdgcn_perm(z, y, 0x07060302u);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < E / 2; ++j) {
+        const int d = E * p.m + (E / 2) * p.half + j;
+        t.v[Tile<D>::v_at(d >> 5, p.u, p.h, d & 31)] = f[j];
+    }
+}
+
+__device__ inline float max_halves(float x)
+{
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// Weights may grow to 2^kSlack times those of the running maximum before the sums are scaled down: most blocks then leave them alone.
+constexpr float kSlack = 8.f;
+
+template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
+{
+    constexpr int S = D / 16, N = D / 32;
+    __shared__ Tile<D> tiles[2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 31, h = lane >> 5;
+    const int item = blockIdx.x;
+    if (item >= a.t.head->n_many * a.n_kv) return;
+    const Entry e = a.t.many[item / a.n_kv];
+    const int hk = item % a.n_kv;
+    const Request r = a.t.request[e.request];
+    int token, head;
+    const bool real = column(r, a.group, a.T, e.tile * kManyCols + wave * 32 + i, token, head);
+    const int limit = real ? r.len + token : -1;
+    const Place pl = place();
+    const int32_t* blocks = a.t.table + (size_t)(r.held >= 0 ? r.row : 0) * a.t.row_blocks;
+    const uint8_t* cache = a.cache + (size_t)hk * Part<D>::kBytes;
+    const size_t stride = (size_t)a.n_kv * Part<D>::kBytes;
+    // (a row that has been released since the plan has no block there)
+    auto part = [&](int b) { return cache + (size_t)min((unsigned)blocks[b], (unsigned)a.t.n_blocks - 1) * stride; };
+
+    u32x4 q[S];
+    {
+        const size_t row = min(r.first + (real ? token : 0), a.T - 1);
+        const uint16_t* p = a.q + row * a.q_stride + ((size_t)hk * a.group + (real ? head : 0)) * D + 8 * h;
+#pragma unroll
+        for (int s = 0; s < S; ++s) q[s] = load16(p + 16 * s);
+    }
+    f32x16 o[N];
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[d][x] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const float scale = a.scale_log2 > 0.f ? a.scale_log2 : 1.f;
+
+    Raw<D> raw;
+    const int end = e.block + e.blocks;
+    if (e.blocks > 0) {
+        load_raw<D>(raw, part(e.block), pl);
+        convert<D>(tiles[0], raw, pl);
+        load_raw<D>(raw, part(min(e.block + 1, end - 1)), pl);
+    }
+    for (int b = e.block, at = 0; b < end; ++b, at ^= 1) {
+        __syncthreads();                               // this block's tile is complete, and the other one has been read
+        if (b + 1 < end) {
+            convert<D>(tiles[at ^ 1], raw, pl);
+            load_raw<D>(raw, part(min(b + 2, end - 1)), pl);
+        }
+        const Tile<D>& t = tiles[at];
+        f32x16 s[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) s[k][x] = 0.f;
+#pragma unroll
+            for (int j = 0; j < S; ++j) s[k] = mfma32(as_bf16x8(t.k[Tile<D>::k_at(k, j, h, i)]), as_bf16x8(q[j]), s[k]);
+        }
+        // (a positive scale is applied in the exponent below; it keeps the order of the scores)
+        if (a.scale_log2 <= 0.f) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) s[k] *= a.scale_log2;
+        }
+        if (b * kBlock + kBlock - 1 > r.len) {         // some column may not see the whole block
+            const int room = limit - b * kBlock - 4 * h;
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int x = 0; x < 16; ++x)
+                    if (32 * k + 8 * (x / 4) + x % 4 > room) s[k][x] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) top = fmaxf(top, s[k][x]);
+        top = max_halves(top) * scale;
+        if (__any(top > m + kSlack)) {
+            const float grown = fmaxf(m, top);
+            const float down = exp2_fast(m - (grown == -INFINITY ? 0.f : grown));
+            l *= down;
+#pragma unroll
+            for (int d = 0; d < N; ++d) o[d] *= down;
+            m = grown;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        u32x4 w[4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int x = 0; x < 16; x += 2) {
+                const float p0 = exp2_fast(__builtin_fmaf(s[k][x], scale, -base)), p1 = exp2_fast(__builtin_fmaf(s[k][x + 1], scale, -base));
+                l += p0 + p1;
+                w[2 * k + x / 8][(x % 8) / 2] = pack_bf16(p0, p1);
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int d = 0; d < N; ++d) o[d] = mfma32(as_bf16x8(t.v[Tile<D>::v_at(d, u, h, i)]), as_bf16x8(w[u]), o[d]);
+    }
+    l += __shfl_xor(l, 32);
+    if (!real) return;
+    if (e.part >= 0) {
+        const size_t slot = ((size_t)e.part * a.n_kv + hk) * kManyCols + wave * 32 + i;
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(a.many_acc + slot * D + 32 * d + 8 * g + 4 * h) = f32x4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+        if (h == 0) {
+            a.many_ml[slot * 2] = m;
+            a.many_ml[slot * 2 + 1] = l;
+        }
+    } else {
+        const float f = l == 0.f ? 0.f : 1.0f / l;
+        uint16_t* out = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)hk * a.group + head) * D + 4 * h;
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<u32x2*>(out + 32 * d + 8 * g) =
+                    u32x2{pack_bf16(o[d][4 * g] * f, o[d][4 * g + 1] * f), pack_bf16(o[d][4 * g + 2] * f, o[d][4 * g + 3] * f)};
+    }
+}
+
+// The partial results of tiles that were cut along their keys.  D / 4 lanes take a column, four dimensions each; where there are many
+// pieces eight groups of lanes share them.
+template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs a)
+{
+    constexpr int L = D / 4, GROUPS = 256 / L;
+    __shared__ float sAcc[GROUPS][D], sL[GROUPS];
+    const int tid = threadIdx.x, lane = tid % L, group = tid / L;
+    const int n_items = a.t.head->n_merge * a.n_kv;
+    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+        const Merge g = a.t.merge[item / a.n_kv];
+        const int h = item % a.n_kv, splits = abs(g.splits), cols = g.splits < 0 ? kManyCols : kFewCols;
+        const float* part_acc = g.splits < 0 ? a.many_acc : a.few_acc;
+        const float* part_ml = g.splits < 0 ? a.many_ml : a.few_ml;
+        const Request r = a.t.request[g.request];
+        const bool share = splits >= 2 * GROUPS;
+        const size_t slot0 = ((size_t)g.part * a.n_kv + h) * cols, step = (size_t)a.n_kv * cols;
+        for (int c0 = blockIdx.y * (share ? 1 : GROUPS); c0 < cols; c0 += gridDim.y * (share ? 1 : GROUPS)) {
+            const int c = share ? c0 : c0 + group;
+            int token, head;
+            const bool real = column(r, a.group, a.T, g.tile * cols + c, token, head);
+            if (share && !real) break;                 // (the same for the whole workgroup; later columns are no more real)
+            float m = -INFINITY, l = 0.f;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+            const float* ml = part_ml + 2 * (slot0 + c);
+            if (real)
+                for (int s = share ? lane : 0; s < splits; s += share ? L : 1) m = fmaxf(m, ml[2 * step * s]);
+            if (share)
+                for (int d = 1; d < L; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+            const float base = m == -INFINITY ? 0.f : m;
+            if (real) {
+                const float* p = part_acc + (slot0 + c) * D + 4 * lane;
+#pragma unroll 4
+                for (int s = share ? group : 0; s < splits; s += share ? GROUPS : 1) {
+                    const float f = exp2_fast(ml[2 * step * s] - base);
+                    l += f * ml[2 * step * s + 1];
+                    acc += f * *reinterpret_cast<const f32x4*>(p + step * D * s);
+                }
+            }
+            if (share) {
+                __syncthreads();
+                *reinterpret_cast<f32x4*>(&sAcc[group][4 * lane]) = acc;
+                if (lane == 0) sL[group] = l;
+                __syncthreads();
+                acc = f32x4{0.f, 0.f, 0.f, 0.f};
+                l = 0.f;
+#pragma unroll
+                for (int w = 0; w < GROUPS; ++w) {
+                    acc += *reinterpret_cast<const f32x4*>(&sAcc[w][4 * lane]);
+                    l += sL[w];
+                }
+            }
+            if (!real || (share && group)) continue;
+            const float f = l == 0.f ? 0.f : 1.0f / l;
+            uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + 4 * lane;
+            *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16(acc[0] * f, acc[1] * f), pack_bf16(acc[2] * f, acc[3] * f)};
+        }
+    }
+}
+
+template <int D> hipError_t attend(const AttendArgs& a, int n_cus, long most_few, long most_many, hipStream_t stream)
+{
+    if (most_many > 0) attend_many_kernel<D><<<(unsigned)(most_many * a.n_kv), 256, 0, stream>>>(a);
+    const int grid = (int)std::max<long>(1, std::min<long>(most_few * a.n_kv, 4L * n_cus));
     attend_few_kernel<D><<<grid, 256, 0, stream>>>(a);
-    merge_kernel<D><<<grid, 256, 0, stream>>>(a);
+    merge_kernel<D><<<dim3(n_cus / 4, 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attend(const AttendArgs& a, int dim, int n_cus, long max_entries, hipStream_t stream)
+hipError_t launch_attend(const AttendArgs& a, int dim, int n_cus, long most_few, long most_many, hipStream_t stream)
 {
     if (a.T == 0) return hipSuccess;
-    return dim == 64 ? attend<64>(a, n_cus, max_entries, stream) : attend<128>(a, n_cus, max_entries, stream);
+    return dim == 64 ? attend<64>(a, n_cus, most_few, most_many, stream) : attend<128>(a, n_cus, most_few, most_many, stream);
 }
 
 }  // namespace kv

@@ -20,9 +20,13 @@ constexpr int kMaxSeqTokens = 1 << 24;
 constexpr int kMaxTokens = 1 << 20;
 constexpr int kMaxHeads = 1024;
 constexpr int kPlanThreads = 1024;
-constexpr int kFewCols = 16;           // columns (token, query head of a key head) of a tile
-// Work items that a launch of attention is cut into at most, apart from one per tile (see plan_kernel).
-constexpr int kFewItems = 2048;
+// Attention works on tiles of columns (token, query head of a key head).  Requests of up to kFewMost columns take tiles of
+// kFewCols, whose waves each convert the codes that they need; longer ones take tiles of kManyCols, whose waves share them.
+constexpr int kFewCols = 16, kManyCols = 128;
+constexpr int kFewMost = 32;
+// Pieces that the keys of the tiles are cut into, over all tiles and key heads; at most one more per tile (see plan_kernel).
+constexpr int kFewItems = 2048, kManyItems = 512;
+constexpr int kFewChunk = 4, kManyChunk = 8;   // blocks of the smallest piece
 constexpr int kMinExp = -100, kMaxExp = 125;
 
 // Bits of the device flag word (LORA_KV_FLAG_*).
@@ -65,7 +69,8 @@ struct Request {
     int32_t entry;     // its first work entry
     int32_t part;      // its first partial result (splits > 1)
     int32_t merge;     // its first merge entry (splits > 1)
-    int32_t pad_[3];
+    int32_t many;      // its tiles have kManyCols columns
+    int32_t pad_[2];
 };
 
 // A piece of a step's attention: a tile of columns against a range of blocks, for every key head.
@@ -82,15 +87,16 @@ struct Merge {
     int32_t request;
     int32_t tile;
     int32_t part;
-    int32_t splits;
+    int32_t splits;    // negative: a tile of kManyCols columns
 };
 
 struct Header {
     uint32_t flags;
     int32_t rows;      // token rows of the step that belong to a request
     int32_t n_few;     // work entries
+    int32_t n_many;
     int32_t n_merge;
-    int32_t pad_[60];
+    int32_t pad_[59];
 };
 
 struct Tables {
@@ -104,6 +110,7 @@ struct Tables {
     int32_t* slot;     // [T], -1: likewise
     Request* request;  // [n]
     Entry* few;
+    Entry* many;
     Merge* merge;
     int32_t n_blocks, n_words, max_seqs, row_blocks, max_seq_tokens;
 };
@@ -147,8 +154,8 @@ struct AttendArgs {
     const uint16_t* q;
     uint16_t* out;
     int64_t q_stride, out_stride;
-    float* part_acc;                    // [slot][kFewCols][D]
-    float* part_ml;                     // [slot][kFewCols][2]
+    float *few_acc, *few_ml;            // partial results: [part][key head][kFewCols][D] and [..][2] (m, l)
+    float *many_acc, *many_ml;          // likewise with kManyCols
     float scale_log2;                   // scale * log2(e)
     int32_t T, n_kv, group;
 };
@@ -157,7 +164,8 @@ hipError_t launch_plan(const PlanArgs& a, hipStream_t stream);
 hipError_t launch_release(const Tables& t, int n, const int32_t* seq, const int32_t* keep, hipStream_t stream);
 hipError_t launch_heads(const HeadsArgs& a, int dim, hipStream_t stream);
 hipError_t launch_read(const ReadArgs& a, int dim, hipStream_t stream);
-hipError_t launch_attend(const AttendArgs& a, int dim, int n_cus, long max_entries, hipStream_t stream);
+// most_few, most_many: entries that the lists can have
+hipError_t launch_attend(const AttendArgs& a, int dim, int n_cus, long most_few, long most_many, hipStream_t stream);
 
 }  // namespace kv
 }  // namespace lora

@@ -51,8 +51,8 @@ __device__ inline void scan(int (&v)[N], int (&total)[N], int (*sums)[N])
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
 {
     __shared__ int claim[kMaxSeqs];
-    __shared__ int sums[kWaves][4];
-    __shared__ unsigned long long work;
+    __shared__ int sums[kWaves][5];
+    __shared__ unsigned long long work[2];
     const int tid = threadIdx.x;
     const Tables& t = a.t;
     const int n = a.n, T = a.T;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
 
     // a row named twice belongs to the first request that names it
     for (int r = tid; r < t.max_seqs; r += kPlanThreads) claim[r] = n;
-    if (tid == 0) work = 0;
+    if (tid < 2) work[tid] = 0;
     __syncthreads();
     for (int i = tid; i < n; i += kPlanThreads) {
         const int row = a.seq[i];
@@ -132,22 +132,25 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
 
     // who gets them; how much attention has to read
     int taken = 0;
-    unsigned long long mine = 0;
+    unsigned long long mine0 = 0, mine1 = 0;
     for (int i = tid; i < n; i += kPlanThreads) {
         Request q = t.request[i];
-        q.tiles = (q.rows * a.group + kFewCols - 1) / kFewCols;
+        q.many = q.rows * a.group > kFewMost;
+        q.tiles = q.many ? (q.rows * a.group + kManyCols - 1) / kManyCols : (q.rows * a.group + kFewCols - 1) / kFewCols;
         if (q.held >= 0) {
             if (q.want > q.held && q.fresh + (q.want - q.held) > found) {
                 flags |= kFlagExhausted;
                 q.held = -1;
             } else {
                 taken = max(taken, q.want > q.held ? q.fresh + (q.want - q.held) : 0);
-                mine += (unsigned long long)q.tiles * (unsigned)((q.len + q.rows + kBlock - 1) / kBlock);
+                const unsigned long long w = (unsigned long long)q.tiles * (unsigned)((q.len + q.rows + kBlock - 1) / kBlock);
+                (q.many ? mine1 : mine0) += w;
             }
         }
         t.request[i] = q;
     }
-    if (mine) atomicAdd(&work, mine);
+    if (mine0) atomicAdd(&work[0], mine0);
+    if (mine1) atomicAdd(&work[1], mine1);
     for (int d = 32; d; d >>= 1) taken = max(taken, __shfl_xor(taken, d));
     __syncthreads();
     if ((tid & 63) == 0) sums[tid >> 6][0] = taken;
@@ -160,38 +163,45 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
         atomicOr(&t.used[b >> 5], 1u << (b & 31));
     }
 
-    // pieces of attention: every tile's keys are cut so that all tiles and key heads together make kFewItems pieces, and at most one more
-    // per tile; the four waves of a workgroup take a piece's blocks in turn
-    const unsigned long long per = (work * a.n_kv + kFewItems - 1) / kFewItems;
-    const int chunk = ((int)(per < 4 ? 4 : per > kMaxBlocks ? kMaxBlocks : per) + 3) & ~3;
-    int e0 = 0, p0 = 0, m0 = 0;
+    // pieces of attention: the keys of every tile are cut so that all tiles and key heads together make kFewItems (kManyItems) pieces, and
+    // at most one more per tile
+    auto cut = [&](unsigned long long w, int items, int least) {
+        const unsigned long long per = (w * a.n_kv + items - 1) / items;
+        return ((int)(per < (unsigned)least ? least : per > kMaxBlocks ? kMaxBlocks : per) + 3) & ~3;
+    };
+    const int chunk0 = cut(work[0], kFewItems, kFewChunk), chunk1 = cut(work[1], kManyItems, kManyChunk);
+    int at[5] = {0, 0, 0, 0, 0};                       // entries, partial results (few, many), merges
     for (int base = 0; base < n; base += kPlanThreads) {
         const int i = base + tid;
         Request q = {};
-        int v[3] = {0, 0, 0}, total[3];
+        int v[5] = {0, 0, 0, 0, 0}, total[5];
         if (i < n) {
             q = t.request[i];
             const int blocks = q.held >= 0 ? (q.len + q.rows + kBlock - 1) / kBlock : 0;
+            const int chunk = q.many ? chunk1 : chunk0;
             q.splits = max(1, (blocks + chunk - 1) / chunk);
             q.chunk = (blocks + q.splits - 1) / q.splits;
-            v[0] = q.tiles * q.splits;
-            v[1] = q.splits > 1 ? q.tiles * q.splits : 0;
-            v[2] = q.splits > 1 ? q.tiles : 0;
+            const int pieces = q.tiles * q.splits;
+            v[0] = q.many ? 0 : pieces;
+            v[1] = q.many ? pieces : 0;
+            v[2] = q.splits > 1 ? v[0] : 0;
+            v[3] = q.splits > 1 ? v[1] : 0;
+            v[4] = q.splits > 1 ? q.tiles : 0;
         }
-        scan<3>(v, total, reinterpret_cast<int(*)[3]>(sums));
+        scan<5>(v, total, sums);
         if (i < n) {
-            q.entry = e0 + v[0];
-            q.part = p0 + v[1];
-            q.merge = m0 + v[2];
+            q.entry = q.many ? at[1] + v[1] : at[0] + v[0];
+            q.part = q.many ? at[3] + v[3] : at[2] + v[2];
+            q.merge = at[4] + v[4];
             t.request[i] = q;
         }
-        e0 += total[0];
-        p0 += total[1];
-        m0 += total[2];
+#pragma unroll
+        for (int k = 0; k < 5; ++k) at[k] += total[k];
     }
     if (tid == 0) {
-        t.head->n_few = e0;
-        t.head->n_merge = m0;
+        t.head->n_few = at[0];
+        t.head->n_many = at[1];
+        t.head->n_merge = at[4];
     }
     if (flags) atomicOr(&t.head->flags, flags);
 }
@@ -219,20 +229,24 @@ __global__ __launch_bounds__(256) void fill_kernel(PlanArgs a)
         for (int b = q.held + (int)threadIdx.x; b < q.want; b += 256) row[b] = t.fresh[q.fresh + b - q.held];
         if (threadIdx.x == 0) t.held[q.row] = q.want;
     }
+    // the last tiles see the most keys: they come first
+    const int cols = q.many ? kManyCols : kFewCols;
+    Entry* list = q.many ? t.many : t.few;
     for (int k = threadIdx.x; k < q.tiles * q.splits; k += 256) {
         Entry e = {};
         e.request = blockIdx.x;
-        e.tile = k / q.splits;
+        e.tile = q.tiles - 1 - k / q.splits;
         e.block = (k % q.splits) * q.chunk;
         // the last token of the tile sees this many blocks
-        const int last = min(q.rows - 1, ((e.tile + 1) * kFewCols - 1) / a.group);
+        const int last = min(q.rows - 1, ((e.tile + 1) * cols - 1) / a.group);
         const int seen = q.held >= 0 ? (q.len + last) / kBlock + 1 : 0;
         e.blocks = max(0, min(q.chunk, seen - e.block));
         e.part = q.splits > 1 ? q.part + k : -1;
-        t.few[q.entry + k] = e;
+        list[q.entry + k] = e;
     }
     if (q.splits > 1)
-        for (int k = threadIdx.x; k < q.tiles; k += 256) t.merge[q.merge + k] = Merge{(int)blockIdx.x, k, q.part + k * q.splits, q.splits};
+        for (int k = threadIdx.x; k < q.tiles; k += 256)
+            t.merge[q.merge + k] = Merge{(int)blockIdx.x, q.tiles - 1 - k, q.part + k * q.splits, q.many ? -q.splits : q.splits};
 }
 
 __global__ __launch_bounds__(64) void release_kernel(Tables t, const int32_t* seq, const int32_t* keep)
