@@ -46,7 +46,7 @@ struct Layout {
 
 // Entries that the lists of a step of T tokens in n requests can have: one a tile, and at most kFewItems (kManyItems) more, counted
 // with the key heads, where tiles are cut along their keys.
-long most_few(long n, int n_kv) { return n * (kFewMost / kFewCols) + kFewItems / n_kv + 1; }
+long most_few(long T, long n, int group, int n_kv) { return T * group / kFewCols + n + kFewItems / n_kv + 1; }
 long most_many(long T, long n, int group, int n_kv) { return T * group / kManyCols + std::min(n, T * group / kFewMost) + kManyItems / n_kv + 1; }
 
 Layout make_layout(const lora_kv_config* c)
@@ -67,10 +67,10 @@ Layout make_layout(const lora_kv_config* c)
     L.slot = take(4 * T);
     L.request = take(sizeof(Request) * seqs);
     const int n_kv = c->n_kv_heads;
-    const size_t few = (size_t)most_few(seqs, n_kv), many = (size_t)most_many(T, seqs, (int)group, n_kv);
+    const size_t few = (size_t)most_few(T, seqs, (int)group, n_kv), many = (size_t)most_many(T, seqs, (int)group, n_kv);
     L.few = take(sizeof(Entry) * few);
     L.many = take(sizeof(Entry) * many);
-    L.merge = take(sizeof(Merge) * (few + many));
+    L.merge = take(sizeof(Merge) * (T * group / kMergeCols + seqs));
     // a cut tile has a partial result per piece, and its pieces are at least half of what a cut is aimed at; nor are there more than the
     // smallest pieces make
     auto parts = [&](size_t items, size_t entries, int least) {
@@ -149,6 +149,7 @@ struct lora_kv {
     bool have_last = false;
     uint64_t epoch = 0;             // of the latest lora_kv_extend / lora_kv_release
     int32_t step_n = -1, step_T = -1;   // of the latest step, -1: none, or ended by a release
+    int32_t step_most = 0;              // no request of it has more new tokens
 
     template <typename Tp> Tp* at(size_t off) const { return reinterpret_cast<Tp*>(base + off); }
     uint8_t* layer(int l) const { return at<uint8_t>(L.cache + L.layer_bytes * (size_t)l); }
@@ -267,6 +268,7 @@ lora_status lora_kv_extend(lora_kv* k, int32_t n, const int32_t* d_seq, const in
     if (KV_HIP_FAIL(launch_plan(a, s))) return LORA_ERR_HIP;
     k->step_n = n;
     k->step_T = T;
+    k->step_most = a.max_new;
     out->start = a.t.start;
     out->position = a.t.position;
     out->slot = a.t.slot;
@@ -346,8 +348,9 @@ lora_status lora_kv_attend(lora_kv* k, int32_t layer, const lora_kv_step* step, 
     a.T = step->T;
     a.n_kv = k->cfg.n_kv_heads;
     a.group = k->cfg.n_heads / k->cfg.n_kv_heads;
-    const long few = most_few(step->n, a.n_kv), many = most_many(step->T, step->n, a.group, a.n_kv);
-    return KV_HIP_FAIL(launch_attend(a, k->cfg.head_dim, k->n_cus, few, (long)step->T * a.group > kFewMost ? many : 0, s)) ? LORA_ERR_HIP : LORA_OK;
+    const long few = most_few(step->T, step->n, a.group, a.n_kv);
+    const long many = (long)k->step_most * a.group > kFewMost ? most_many(step->T, step->n, a.group, a.n_kv) : 0;
+    return KV_HIP_FAIL(launch_attend(a, k->cfg.head_dim, k->n_cus, few, many, s)) ? LORA_ERR_HIP : LORA_OK;
 }
 
 lora_status lora_kv_read(lora_kv* k, int32_t layer, int32_t n, const int32_t* d_seq, const int32_t* d_position, void* d_k_out, void* d_v_out,

@@ -49,12 +49,16 @@ template <int W> __device__ inline void load_words(uint32_t (&d)[W], const uint8
     }
 }
 
-template <int D> __device__ inline void load_block(Codes<D>& c, const uint8_t* part, int lane)
+template <int D> __device__ inline void load_keys(Codes<D>& c, const uint8_t* part, int lane)
 {
     const int m = lane & 15, quad = lane >> 4;
 #pragma unroll
     for (int t = 0; t < 4; ++t) load_words(c.k[t], part + Part<D>::kK + (16 * t + m) * Part<D>::kRow + quad * (D / 8));
     c.ke = *reinterpret_cast<const uint32_t*>(part + Part<D>::kKExp + Part<D>::k_exp_at(m, quad * (D / 4) / kGroup));
+}
+template <int D> __device__ inline void load_values(Codes<D>& c, const uint8_t* part, int lane)
+{
+    const int m = lane & 15, quad = lane >> 4;
 #pragma unroll
     for (int t = 0; t < 4; ++t) load_words(c.v[t], part + Part<D>::kV + Part<D>::v_at(16 * t + 4 * quad, m * Part<D>::kE));
     c.ve = *reinterpret_cast<const u32x4*>(part + Part<D>::kVExp + Part<D>::v_exp_at(4 * quad, m * Part<D>::kE / kGroup));
@@ -67,12 +71,14 @@ template <int D> struct Running {
     f32x4 acc[D / 16];
 };
 
-// One block of 64 keys.  limit: the last key position of the lane's column, relative to the block's first; masked: some column does
-// not see the whole block.
-template <int D> __device__ inline void one_block(Running<D>& r, const Codes<D>& c, const u32x4 (&q)[D / 32], float scale_log2, int limit, bool masked,
-                                                  int quad)
+// One block of 64 keys, and the request for the codes of the wave's next one (at `next`) as soon as this one's have been used: keys
+// travel during the second half of the block, values during the first half of the next.  limit: the last key position of the lane's
+// column, relative to the block's first; masked: some column does not see the whole block.
+template <int D> __device__ inline void one_block(Running<D>& r, Codes<D>& c, const u32x4 (&q)[D / 32], float scale_log2, int limit, bool masked,
+                                                  const uint8_t* next, int lane)
 {
     constexpr int S = D / 32;
+    const int quad = lane >> 4;
     f32x4 s[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -81,6 +87,7 @@ template <int D> __device__ inline void one_block(Running<D>& r, const Codes<D>&
 #pragma unroll
         for (int k = 0; k < S; ++k) s[t] = mfma16(eight_bf16(c.k[t][k], e), q[k], s[t]);
     }
+    load_keys<D>(c, next, lane);
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -144,6 +151,7 @@ template <int D> __device__ inline void one_block(Running<D>& r, const Codes<D>&
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) r.acc[j] = mfma16(f[j], w, r.acc[j]);
     }
+    load_values<D>(c, next, lane);
 }
 
 // Token and head that a request's column is; false: there is none in the step.
@@ -154,7 +162,7 @@ __device__ inline bool column(const Request& r, int group, int T, int col, int& 
     return token < r.rows && r.first + token < T;
 }
 
-template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a)
+template <int D> __global__ __launch_bounds__(256, 3) void attend_few_kernel(AttendArgs a)
 {
     constexpr int kPad = 4;
     __shared__ float sAcc[4][kFewCols][D + kPad];
@@ -182,12 +190,23 @@ template <int D> __global__ __launch_bounds__(256) void attend_few_kernel(Attend
             for (int k = 0; k < D / 32; ++k) q[k] = load16(p + 8 * k);
         }
         const int32_t* blocks = a.t.table + (size_t)(r.held >= 0 ? r.row : 0) * a.t.row_blocks;
-        for (int b = e.block + wave; b < e.block + e.blocks; b += 4) {
-            // (a row that has been released since the plan has no block there)
-            const int at = min((unsigned)blocks[b], (unsigned)a.t.n_blocks - 1);
+        // (a row that has been released since the plan has no block there)
+        auto part = [&](int b) {
+            return a.cache + ((size_t)min((unsigned)blocks[b], (unsigned)a.t.n_blocks - 1) * a.n_kv + h) * Part<D>::kBytes;
+        };
+        const int end = e.block + e.blocks;
+        int b = e.block + wave;
+        if (b < end) {
             Codes<D> codes;
-            load_block<D>(codes, a.cache + ((size_t)at * a.n_kv + h) * Part<D>::kBytes, lane);
-            one_block<D>(run, codes, q, a.scale_log2, limit - b * kBlock, b * kBlock + kBlock - 1 > r.len, quad);
+            const uint8_t* next = part(b);
+            load_keys<D>(codes, next, lane);
+            load_values<D>(codes, next, lane);
+            next = part(min(b + 4, end - 1));
+            for (; b < end; b += 4) {
+                const uint8_t* after = part(min(b + 8, end - 1));
+                one_block<D>(run, codes, q, a.scale_log2, limit - b * kBlock, b * kBlock + kBlock - 1 > r.len, next, lane);
+                next = after;
+            }
         }
         // the four waves' results
         run.l += __shfl_xor(run.l, 16);
@@ -443,8 +462,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
     }
 }
 
-// The partial results of tiles that were cut along their keys.  D / 4 lanes take a column, four dimensions each; where there are many
-// pieces eight groups of lanes share them.
+// The partial results of tiles that were cut along their keys.  D / 4 lanes take a column, four dimensions each.  Where there are many
+// pieces, a workgroup's groups of lanes share those of one column (blockIdx.y).
 template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs a)
 {
     constexpr int L = D / 4, GROUPS = 256 / L;
@@ -457,29 +476,25 @@ template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs 
         const float* part_acc = g.splits < 0 ? a.many_acc : a.few_acc;
         const float* part_ml = g.splits < 0 ? a.many_ml : a.few_ml;
         const Request r = a.t.request[g.request];
-        const bool share = splits >= 2 * GROUPS;
-        const size_t slot0 = ((size_t)g.part * a.n_kv + h) * cols, step = (size_t)a.n_kv * cols;
-        for (int c0 = blockIdx.y * (share ? 1 : GROUPS); c0 < cols; c0 += gridDim.y * (share ? 1 : GROUPS)) {
-            const int c = share ? c0 : c0 + group;
+        const size_t slot0 = ((size_t)g.part * a.n_kv + h) * cols + g.col % cols, step = (size_t)a.n_kv * cols;
+        const bool share = splits >= 2 * GROUPS;       // (the same for the whole workgroup, like everything but `group` and `lane`)
+        if (!share && blockIdx.y) continue;
+        for (int c = share ? (int)blockIdx.y : group; c < kMergeCols; c += share ? (int)gridDim.y : GROUPS) {
             int token, head;
-            const bool real = column(r, a.group, a.T, g.tile * cols + c, token, head);
-            if (share && !real) break;                 // (the same for the whole workgroup; later columns are no more real)
+            if (!column(r, a.group, a.T, g.col + c, token, head)) break;
             float m = -INFINITY, l = 0.f;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
             const float* ml = part_ml + 2 * (slot0 + c);
-            if (real)
-                for (int s = share ? lane : 0; s < splits; s += share ? L : 1) m = fmaxf(m, ml[2 * step * s]);
+            for (int s = share ? lane : 0; s < splits; s += share ? L : 1) m = fmaxf(m, ml[2 * step * s]);
             if (share)
                 for (int d = 1; d < L; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
             const float base = m == -INFINITY ? 0.f : m;
-            if (real) {
-                const float* p = part_acc + (slot0 + c) * D + 4 * lane;
+            const float* p = part_acc + (slot0 + c) * D + 4 * lane;
 #pragma unroll 4
-                for (int s = share ? group : 0; s < splits; s += share ? GROUPS : 1) {
-                    const float f = exp2_fast(ml[2 * step * s] - base);
-                    l += f * ml[2 * step * s + 1];
-                    acc += f * *reinterpret_cast<const f32x4*>(p + step * D * s);
-                }
+            for (int s = share ? group : 0; s < splits; s += share ? GROUPS : 1) {
+                const float f = exp2_fast(ml[2 * step * s] - base);
+                l += f * ml[2 * step * s + 1];
+                acc += f * *reinterpret_cast<const f32x4*>(p + step * D * s);
             }
             if (share) {
                 __syncthreads();
@@ -493,8 +508,8 @@ template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs 
                     acc += *reinterpret_cast<const f32x4*>(&sAcc[w][4 * lane]);
                     l += sL[w];
                 }
+                if (group) continue;
             }
-            if (!real || (share && group)) continue;
             const float f = l == 0.f ? 0.f : 1.0f / l;
             uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + 4 * lane;
             *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16(acc[0] * f, acc[1] * f), pack_bf16(acc[2] * f, acc[3] * f)};
@@ -505,9 +520,9 @@ template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs 
 template <int D> hipError_t attend(const AttendArgs& a, int n_cus, long most_few, long most_many, hipStream_t stream)
 {
     if (most_many > 0) attend_many_kernel<D><<<(unsigned)(most_many * a.n_kv), 256, 0, stream>>>(a);
-    const int grid = (int)std::max<long>(1, std::min<long>(most_few * a.n_kv, 4L * n_cus));
+    const int grid = (int)std::max<long>(1, std::min<long>(most_few * a.n_kv, 3L * n_cus));
     attend_few_kernel<D><<<grid, 256, 0, stream>>>(a);
-    merge_kernel<D><<<dim3(n_cus / 4, 4), 256, 0, stream>>>(a);
+    merge_kernel<D><<<dim3(4 * n_cus, 4), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -82,11 +82,12 @@ struct Entry {
     int32_t part;      // partial result that it writes, -1: the output itself
     int32_t pad_[3];
 };
-// A tile whose range was split: its partial results are merged behind.
+// Columns whose tile's range was split: the partial results are merged behind.
+constexpr int kMergeCols = 8;
 struct Merge {
     int32_t request;
-    int32_t tile;
-    int32_t part;
+    int32_t col;       // first of kMergeCols columns
+    int32_t part;      // first partial result of their tile
     int32_t splits;    // negative: a tile of kManyCols columns
 };
 

@@ -135,17 +135,21 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
     unsigned long long mine0 = 0, mine1 = 0;
     for (int i = tid; i < n; i += kPlanThreads) {
         Request q = t.request[i];
-        q.many = q.rows * a.group > kFewMost;
-        q.tiles = q.many ? (q.rows * a.group + kManyCols - 1) / kManyCols : (q.rows * a.group + kFewCols - 1) / kFewCols;
         if (q.held >= 0) {
             if (q.want > q.held && q.fresh + (q.want - q.held) > found) {
                 flags |= kFlagExhausted;
                 q.held = -1;
             } else {
                 taken = max(taken, q.want > q.held ? q.fresh + (q.want - q.held) : 0);
-                const unsigned long long w = (unsigned long long)q.tiles * (unsigned)((q.len + q.rows + kBlock - 1) / kBlock);
-                (q.many ? mine1 : mine0) += w;
             }
+        }
+        // (a refused request's rows are set to zero by the kernel of few columns, however many they are)
+        const int cols = q.rows * a.group;
+        q.many = q.held >= 0 && cols > kFewMost;
+        q.tiles = q.many ? (cols + kManyCols - 1) / kManyCols : (cols + kFewCols - 1) / kFewCols;
+        if (q.held >= 0) {
+            const unsigned long long w = (unsigned long long)q.tiles * (unsigned)((q.len + q.rows + kBlock - 1) / kBlock);
+            (q.many ? mine1 : mine0) += w;
         }
         t.request[i] = q;
     }
@@ -164,7 +168,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
     }
 
     // pieces of attention: the keys of every tile are cut so that all tiles and key heads together make kFewItems (kManyItems) pieces, and
-    // at most one more per tile
+    // at most one more per tile; a tile of up to one and a half pieces stays whole
     auto cut = [&](unsigned long long w, int items, int least) {
         const unsigned long long per = (w * a.n_kv + items - 1) / items;
         return ((int)(per < (unsigned)least ? least : per > kMaxBlocks ? kMaxBlocks : per) + 3) & ~3;
@@ -179,14 +183,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
             q = t.request[i];
             const int blocks = q.held >= 0 ? (q.len + q.rows + kBlock - 1) / kBlock : 0;
             const int chunk = q.many ? chunk1 : chunk0;
-            q.splits = max(1, (blocks + chunk - 1) / chunk);
+            q.splits = max(1, (blocks + chunk / 2) / chunk);
             q.chunk = (blocks + q.splits - 1) / q.splits;
             const int pieces = q.tiles * q.splits;
             v[0] = q.many ? 0 : pieces;
             v[1] = q.many ? pieces : 0;
             v[2] = q.splits > 1 ? v[0] : 0;
             v[3] = q.splits > 1 ? v[1] : 0;
-            v[4] = q.splits > 1 ? q.tiles : 0;
+            v[4] = q.splits > 1 ? (q.rows * a.group + kMergeCols - 1) / kMergeCols : 0;
         }
         scan<5>(v, total, sums);
         if (i < n) {
@@ -245,8 +249,10 @@ __global__ __launch_bounds__(256) void fill_kernel(PlanArgs a)
         list[q.entry + k] = e;
     }
     if (q.splits > 1)
-        for (int k = threadIdx.x; k < q.tiles; k += 256)
-            t.merge[q.merge + k] = Merge{(int)blockIdx.x, q.tiles - 1 - k, q.part + k * q.splits, q.many ? -q.splits : q.splits};
+        for (int k = threadIdx.x; k * kMergeCols < q.rows * a.group; k += 256) {
+            const int place = q.tiles - 1 - k * kMergeCols / cols;
+            t.merge[q.merge + k] = Merge{(int)blockIdx.x, k * kMergeCols, q.part + place * q.splits, q.many ? -q.splits : q.splits};
+        }
 }
 
 __global__ __launch_bounds__(64) void release_kernel(Tables t, const int32_t* seq, const int32_t* keep)
