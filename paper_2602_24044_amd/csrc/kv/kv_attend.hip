@@ -27,14 +27,64 @@ __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
 }
 
+// Weights may grow to 2^kSlack times those of the running maximum before the sums are scaled down: most blocks then leave them alone.
+constexpr float kSlack = 8.f;
+
+// The largest over lanes 32 apart, and over lanes 16 and 32 apart: rows of a register change places with rows of its copy on the vector
+// unit.  (The copy is hidden from the compiler, which otherwise takes both results for one and drops the comparison.)
+__device__ inline float max_halves(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    uint32_t v = u;
+    asm("" : "+v"(v));
+    const auto r = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ inline float max_quarters(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    uint32_t v = u;
+    asm("" : "+v"(v));
+    const auto r = __builtin_amdgcn_permlane16_swap(u, v, false, false);
+    return max_halves(fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1])));
+}
+
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int D> struct Codes {
-    static constexpr int W = D / 32;      // dwords of a lane's part of a key tile (32 or 16 codes) and of a value tile
-    uint32_t k[4][W], v[4][W];
-    uint32_t ke;
-    u32x4 ve;
+// ---- tiles of few columns ----
+// A wave takes a piece of a tile by itself, sixteen waves on a CU.  Its blocks are copied to LDS as they are, the next block's keys as
+// soon as this block's scores are there, its values at the end of the block: what is on its way hangs on no register.
+template <int D> struct Stage {
+    static constexpr int kKeys = 2, kExpPlaces = 4;
+    static constexpr int kHalf = kBlock * Part<D>::kRow, kExps = 2 * kBlock * Part<D>::kGroups;
+    static constexpr int kCopies = kHalf / 1024;       // copy instructions of a half; the exponents take one
+    static constexpr int kV = kKeys * kHalf, kE = kV + kHalf, kBytes = kE + kExpPlaces * kExps;
 };
+
+// 16 bytes per active lane, lane * 16 behind `from`, to LDS at lds + 16 * lane.  m0 carries the LDS address (the compiler writes it itself
+// directly in front of its own uses); the copy wants a wait state behind the write.
+__device__ inline void copy16(const uint8_t* from, uint32_t lane16, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane16), "s"(from), "s"(lds) : "memory");
+}
+// All but the wave's latest N requests to memory have come back.
+template <int N> __device__ inline void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// What has been read from LDS is in registers: its place may be overwritten.
+__device__ inline void read_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// lds: where the stage is; b: number of the block in its piece.
+template <int D> __device__ inline void copy_keys(uint32_t lds, int b, const uint8_t* part, int lane)
+{
+    using T = Stage<D>;
+    if (16 * lane < T::kExps) copy16(part + Part<D>::kKExp, 16 * lane, lds + T::kE + b % T::kExpPlaces * T::kExps);
+#pragma unroll
+    for (int c = 0; c < T::kCopies; ++c) copy16(part + Part<D>::kK + 1024 * c, 16 * lane, lds + b % T::kKeys * T::kHalf + 1024 * c);
+}
+template <int D> __device__ inline void copy_values(uint32_t lds, const uint8_t* part, int lane)
+{
+#pragma unroll
+    for (int c = 0; c < Stage<D>::kCopies; ++c) copy16(part + Part<D>::kV + 1024 * c, 16 * lane, lds + Stage<D>::kV + 1024 * c);
+}
 
 template <int W> __device__ inline void load_words(uint32_t (&d)[W], const uint8_t* p)
 {
@@ -49,210 +99,276 @@ template <int W> __device__ inline void load_words(uint32_t (&d)[W], const uint8
     }
 }
 
-template <int D> __device__ inline void load_keys(Codes<D>& c, const uint8_t* part, int lane)
-{
-    const int m = lane & 15, quad = lane >> 4;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) load_words(c.k[t], part + Part<D>::kK + (16 * t + m) * Part<D>::kRow + quad * (D / 8));
-    c.ke = *reinterpret_cast<const uint32_t*>(part + Part<D>::kKExp + Part<D>::k_exp_at(m, quad * (D / 4) / kGroup));
-}
-template <int D> __device__ inline void load_values(Codes<D>& c, const uint8_t* part, int lane)
-{
-    const int m = lane & 15, quad = lane >> 4;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) load_words(c.v[t], part + Part<D>::kV + Part<D>::v_at(16 * t + 4 * quad, m * Part<D>::kE));
-    c.ve = *reinterpret_cast<const u32x4*>(part + Part<D>::kVExp + Part<D>::v_exp_at(4 * quad, m * Part<D>::kE / kGroup));
-}
-
-// Weighted sum of a tile's columns: m and l for the lane's column (l: of the lane's own keys only), acc[j][i]: dimension
-// E (4 quarter + i) + j of the lane's column.
+// m of the lane's column, l[i] the sum of its weights (every i the same: a product with ones, of the weights as they are rounded for
+// the values), acc[j][i]: dimension E (4 quarter + i) + j of it.
 template <int D> struct Running {
-    float m, l;
-    f32x4 acc[D / 16];
+    float m;
+    f32x4 l, acc[D / 16];
 };
 
-// One block of 64 keys, and the request for the codes of the wave's next one (at `next`) as soon as this one's have been used: keys
-// travel during the second half of the block, values during the first half of the next.  limit: the last key position of the lane's
-// column, relative to the block's first; masked: some column does not see the whole block.
-template <int D> __device__ inline void one_block(Running<D>& r, Codes<D>& c, const u32x4 (&q)[D / 32], float scale_log2, int limit, bool masked,
-                                                  const uint8_t* next, int lane)
+// Scores on the MFMA that takes four-bit operands with a power of two for every 32 values, as the cache holds the keys: they need no
+// conversion.  The other operand has eight bits then: a query is taken apart into two e4m3 numbers, q = 2^n (a + b / 16), a the nearest
+// to q / 2^n and b to what is left.  With the largest of the head's values at 2^7 .. 2^8 that is exact for the eight significant bits of bf16
+// down to 2^-14 of it, and off by at most 2^-21 of it below.
+// Lane (column, quarter) of the 16x16x128 MFMA has four-bit operands k = 32 quarter .. + 31 and eight-bit ones k = 16 quarter .. + 15 and
+// 64 + 16 quarter .. + 15; the exponent of operands 32 j .. + 31 comes from quarter j.  With heads of 128, a and b take an MFMA each; with
+// heads of 64, operands 64 .. 127 are b, against the same keys.
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+template <int D> struct Query {
+    static constexpr int kTerms = D / 64;
+    i32x8 x[kTerms];
+    int e[kTerms];                                     // biased exponent
+};
+
+__device__ inline i32x8 four_dwords(u32x4 v)
 {
-    constexpr int S = D / 32;
+    const i32x8 r = {(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+    return r;                                          // (four-bit operands are the first half)
+}
+
+// row: the column's query.
+template <int D> __device__ inline void split_query(Query<D>& q, const uint16_t* row, int lane)
+{
+    constexpr int H = D / 64;                          // 16 dimensions, twice with heads of 128
     const int quad = lane >> 4;
-    f32x4 s[4];
+    u32x4 raw[2 * H];
+#pragma unroll
+    for (int j = 0; j < 2 * H; ++j) raw[j] = load16(row + 64 * (j / 2) + 16 * quad + 8 * (j % 2));
+    float top = 0.f, odd = 0.f;                        // odd: a NaN where a value is a NaN or an infinity, which makes the column one
+#pragma unroll
+    for (int j = 0; j < 2 * H; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = __builtin_fabsf(lo_f32(raw[j][i])), y = __builtin_fabsf(hi_f32(raw[j][i]));
+            odd = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, odd));
+            top = fmaxf(top, fmaxf(x, y));
+        }
+    top = max_quarters(top);
+    const int n = max((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127 - 7, -120);
+    const float down = __builtin_bit_cast(float, (uint32_t)(127 - n) << 23);
+#pragma unroll
+    for (int j = 0; j < 2 * H; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const float y[4] = {__builtin_fmaf(lo_f32(raw[j][i]), down, odd), __builtin_fmaf(hi_f32(raw[j][i]), down, odd),
+                                __builtin_fmaf(lo_f32(raw[j][i + 1]), down, odd), __builtin_fmaf(hi_f32(raw[j][i + 1]), down, odd)};
+            int a = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+            a = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], a, true);
+            const f32x2 a0 = __builtin_amdgcn_cvt_pk_f32_fp8(a, false), a1 = __builtin_amdgcn_cvt_pk_f32_fp8(a, true);
+            int b = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - a0[0]) * 16.f, (y[1] - a0[1]) * 16.f, 0, false);
+            b = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - a1[0]) * 16.f, (y[3] - a1[1]) * 16.f, b, true);
+            q.x[0][2 * j + i / 2] = a;
+            if constexpr (D == 128) q.x[1][2 * j + i / 2] = b;
+            else q.x[0][4 + 2 * j + i / 2] = b;
+        }
+    q.e[0] = n + 127 - (D == 64 && quad >= 2 ? 4 : 0);
+    if constexpr (D == 128) q.e[1] = n + 127 - 4;
+}
+
+// s[t][i]: score of key 16 t + 4 quarter + i of a block.
+template <int D> __device__ inline void scores(f32x4 (&s)[4], const uint8_t* keys, const uint8_t* exps, const Query<D>& q, int lane)
+{
+    const int m = lane & 15, g = D == 128 ? lane >> 4 : (lane >> 4) & 1;
+    const int e = *reinterpret_cast<const int*>(exps + Part<D>::k_exp_at(m, g));
+    i32x8 k[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const uint32_t e = t == 0 ? c.ke << 23 : t == 1 ? c.ke << 15 : t == 2 ? c.ke << 7 : c.ke >> 1;
+        k[t] = four_dwords(*reinterpret_cast<const u32x4*>(keys + (16 * t + m) * Part<D>::kRow + 16 * g));
         s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < S; ++k) s[t] = mfma16(eight_bf16(c.k[t][k], e), q[k], s[t]);
     }
-    load_keys<D>(c, next, lane);
+    // (formats: 4 = e2m1, 0 = e4m3; the number behind is the byte of the exponents)
+#pragma unroll
+    for (int x = 0; x < Query<D>::kTerms; ++x) {
+        s[0] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k[0], q.x[x], s[0], 4, 0, 0, e, 0, q.e[x]);
+        s[1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k[1], q.x[x], s[1], 4, 0, 1, e, 0, q.e[x]);
+        s[2] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k[2], q.x[x], s[2], 4, 0, 2, e, 0, q.e[x]);
+        s[3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k[3], q.x[x], s[3], 4, 0, 3, e, 0, q.e[x]);
+    }
+}
+
+// Weights of a block's scores; limit: the last key position of the lane's column, relative to the block's first; masked: some column does
+// not see the whole block.
+template <int D> __device__ inline void weights(Running<D>& r, uint32_t (&p)[4][2], f32x4 (&s)[4], float scale_log2, int limit, bool masked, int lane)
+{
+    const int quad = lane >> 4;
     float top = -INFINITY;
+    // (a positive scale is applied in the exponent below; it keeps the order of the scores)
+    if (scale_log2 <= 0.f) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] *= scale_log2;
+    }
+    const float scale = scale_log2 > 0.f ? scale_log2 : 1.f;
+    if (masked)
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (16 * t + 4 * quad + i > limit) s[t][i] = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s[t][i] *= scale_log2;
-            if (masked && 16 * t + 4 * quad + i > limit) s[t][i] = -INFINITY;
-            top = fmaxf(top, s[t][i]);
-        }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m = fmaxf(r.m, top);
-    // a column that has seen no key yet keeps m = -inf: its weights are 2^-inf = 0, not 2^(-inf + inf)
-    const float base = m == -INFINITY ? 0.f : m;
-    if (__any(m > r.m)) {
-        const float down = exp2_fast(r.m - base);
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
+    top = max_quarters(top) * scale;
+    if (__any(top > r.m + kSlack)) {
+        const float m = fmaxf(r.m, top);
+        const float down = exp2_fast(r.m - (m == -INFINITY ? 0.f : m));
         r.l *= down;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) r.acc[j] *= down;
         r.m = m;
     }
-    uint32_t p[4][2];
+    // a column that has seen no key yet keeps m = -inf: its weights are 2^-inf = 0, not 2^(-inf + inf)
+    const float base = r.m == -INFINITY ? 0.f : r.m;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         float w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = exp2_fast(s[t][i] - base);
-            r.l += w[i];
+            w[i] = exp2_fast(__builtin_fmaf(s[t][i], scale, -base));
         }
         p[t][0] = pack_bf16(w[0], w[1]);
         p[t][1] = pack_bf16(w[2], w[3]);
     }
-    // V^T of 32 keys: keys 4 quarter .. + 3 of tile 2 h, then of tile 2 h + 1.  A key's codes come two dimensions at a time; two keys'
-    // results are dealt into the two dimensions' operands.
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const u32x4 w = {p[2 * h][0], p[2 * h][1], p[2 * h + 1][0], p[2 * h + 1][1]};
-        u32x4 f[D / 16];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {                  // keys 2 x, 2 x + 1 of the eight
-            const int t = 2 * h + x / 2, i = 2 * (x & 1);
-            const uint32_t e = c.ve[t];
-            const uint32_t e0 = i == 0 ? e << 23 : e << 7, e1 = i == 0 ? e << 15 : e >> 1;
-            auto deal = [&](int d, uint32_t a, uint32_t b) {
-                f[d][x] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-                f[d + 1][x] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-            };
-            if constexpr (D == 128) {
-                const uint32_t a = c.v[t][i], b = c.v[t][i + 1];
-                deal(0, two_bf16<0>(a, e0), two_bf16<0>(b, e1));
-                deal(2, two_bf16<1>(a, e0), two_bf16<1>(b, e1));
-                deal(4, two_bf16<2>(a, e0), two_bf16<2>(b, e1));
-                deal(6, two_bf16<3>(a, e0), two_bf16<3>(b, e1));
-            } else {
-                const uint32_t a = c.v[t][i / 2];      // both keys in one dword, four codes each
-                deal(0, two_bf16<0>(a, e0), two_bf16<2>(a, e1));
-                deal(2, two_bf16<1>(a, e0), two_bf16<3>(a, e1));
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < D / 16; ++j) r.acc[j] = mfma16(f[j], w, r.acc[j]);
-    }
-    load_values<D>(c, next, lane);
 }
 
-// Token and head that a request's column is; false: there is none in the step.
-__device__ inline bool column(const Request& r, int group, int T, int col, int& token, int& head)
+// The weighted values of 64 keys.  V^T of 32 keys: keys 4 quarter .. + 3 of tile 2 h, then of tile 2 h + 1.  A key's codes come two
+// dimensions at a time; two keys' results are dealt into the two dimensions' operands.
+template <int D> __device__ inline void add_values(Running<D>& r, const uint32_t (&p)[4][2], const uint8_t* values, const uint8_t* exps, int lane)
+{
+    constexpr int W = D / 32;
+    const int m = lane & 15, quad = lane >> 4;
+    const u32x4 ve = *reinterpret_cast<const u32x4*>(exps + kBlock * Part<D>::kGroups + Part<D>::v_exp_at(4 * quad, m * Part<D>::kE / kGroup));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t c[2][W];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) load_words(c[t], values + Part<D>::v_at(16 * (2 * h + t) + 4 * quad, m * Part<D>::kE));
+        const u32x4 w = {p[2 * h][0], p[2 * h][1], p[2 * h + 1][0], p[2 * h + 1][1]};
+        r.l = mfma16(u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, w, r.l);
+#pragma unroll
+        for (int d = 0; d < D / 16; d += 4) {          // four dimensions at a time: 16 registers of operands
+            u32x4 f[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {              // keys 2 x, 2 x + 1 of the eight
+                const int t = x / 2, i = 2 * (x & 1);
+                const uint32_t e = ve[2 * h + t];
+                const uint32_t e0 = i == 0 ? e << 23 : e << 7, e1 = i == 0 ? e << 15 : e >> 1;
+                auto deal = [&](int j, uint32_t a, uint32_t b) {
+                    f[j][x] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                    f[j + 1][x] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                };
+                if constexpr (D == 128) {
+                    const uint32_t a = c[t][i], b = c[t][i + 1];
+                    deal(0, d == 0 ? two_bf16<0>(a, e0) : two_bf16<2>(a, e0), d == 0 ? two_bf16<0>(b, e1) : two_bf16<2>(b, e1));
+                    deal(2, d == 0 ? two_bf16<1>(a, e0) : two_bf16<3>(a, e0), d == 0 ? two_bf16<1>(b, e1) : two_bf16<3>(b, e1));
+                } else {
+                    const uint32_t a = c[t][i / 2];    // both keys in one dword, four codes each
+                    deal(0, two_bf16<0>(a, e0), two_bf16<2>(a, e1));
+                    deal(2, two_bf16<1>(a, e0), two_bf16<3>(a, e1));
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.acc[d + j] = mfma16(f[j], w, r.acc[d + j]);
+        }
+    }
+}
+
+// Token and head that a request's (an entry's) column is; false: there is none in the step.
+template <typename Of> __device__ inline bool column(const Of& r, int group, int T, int col, int& token, int& head)
 {
     token = col / group;
     head = col - token * group;
     return token < r.rows && r.first + token < T;
 }
 
-template <int D> __global__ __launch_bounds__(256, 3) void attend_few_kernel(AttendArgs a)
+template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(AttendArgs a)
 {
-    constexpr int kPad = 4;
-    __shared__ float sAcc[4][kFewCols][D + kPad];
-    __shared__ float sM[4][kFewCols], sL[4][kFewCols];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int c = lane & 15, quad = lane >> 4;
-    const int n_items = a.t.head->n_few * a.n_kv;
-    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
-        const Entry e = a.t.few[item / a.n_kv];
+    using St = Stage<D>;
+    constexpr int A = St::kCopies + 1, B = St::kCopies;             // requests for a block's keys (with the exponents), and for its values
+    __shared__ __align__(1024) uint8_t stage[St::kBytes];
+    const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)stage;
+    const int lane = threadIdx.x, c = lane & 15, quad = lane >> 4;
+    for (int item = blockIdx.x; item < a.n_few * a.n_kv; item += gridDim.x) {
+        const Entry& r = a.t.few[item / a.n_kv];
+        if (r.rows == 0) return;
         const int h = item % a.n_kv;
-        const Request r = a.t.request[e.request];
         int token, head;
-        const bool real = column(r, a.group, a.T, e.tile * kFewCols + c, token, head);
-        const int limit = r.len + token;                                    // last key that the lane's column sees
+        const bool real = column(r, a.group, a.T, r.tile * kFewCols + c, token, head);
+        const int limit = r.len + token;                            // last key that the lane's column sees
+        const int32_t* blocks = a.t.table + (size_t)r.row * a.t.row_blocks + r.block;
+        const int n = r.blocks, first = r.block, len = r.len;
         Running<D> run;
         run.m = -INFINITY;
-        run.l = 0.f;
+        run.l = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) run.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        u32x4 q[D / 32];
-        {
-            const size_t row = min(r.first + (real ? token : 0), a.T - 1);
-            const uint16_t* p = a.q + row * a.q_stride + ((size_t)h * a.group + head) * D + quad * (D / 4);
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) q[k] = load16(p + 8 * k);
-        }
-        const int32_t* blocks = a.t.table + (size_t)(r.held >= 0 ? r.row : 0) * a.t.row_blocks;
-        // (a row that has been released since the plan has no block there)
-        auto part = [&](int b) {
-            return a.cache + ((size_t)min((unsigned)blocks[b], (unsigned)a.t.n_blocks - 1) * a.n_kv + h) * Part<D>::kBytes;
-        };
-        const int end = e.block + e.blocks;
-        int b = e.block + wave;
-        if (b < end) {
-            Codes<D> codes;
-            const uint8_t* next = part(b);
-            load_keys<D>(codes, next, lane);
-            load_values<D>(codes, next, lane);
-            next = part(min(b + 4, end - 1));
-            for (; b < end; b += 4) {
-                const uint8_t* after = part(min(b + 8, end - 1));
-                one_block<D>(run, codes, q, a.scale_log2, limit - b * kBlock, b * kBlock + kBlock - 1 > r.len, next, lane);
+        if (n > 0) {
+            // 64 block numbers at a time, one per lane; behind those that came with the entry they are fetched meanwhile.  (A row that has
+            // been released since the plan has none: any block will do.)
+            uint32_t ids = r.id[lane & (kEntryIds - 1)];
+            auto part = [&](int b) {
+                if (b == kEntryIds || (b && b % 64 == 0))
+                    ids = min((unsigned)blocks[min((b & ~63) + lane, n - 1)], (unsigned)a.t.n_blocks - 1);
+                const uint32_t at = __builtin_amdgcn_readlane(ids, b & 63);
+                return a.cache + ((size_t)at * a.n_kv + h) * Part<D>::kBytes;
+            };
+            const uint8_t *now = part(0), *next = now;
+            copy_keys<D>(lds, 0, now, lane);
+            if (n > 1) {
+                next = part(1);
+                copy_keys<D>(lds, 1, next, lane);
+            }
+            copy_values<D>(lds, now, lane);
+            Query<D> q;
+            split_query<D>(q, a.q + (size_t)min(r.first + (real ? token : 0), a.T - 1) * a.q_stride + ((size_t)h * a.group + (real ? head : 0)) * D, lane);
+            for (int b = 0; b < n; ++b) {
+                const bool one_more = b + 1 < n, two_more = b + 2 < n;
+                const int at = (first + b) * kBlock;
+                const uint8_t* exps = stage + St::kE + b % St::kExpPlaces * St::kExps;
+                if (one_more) landed<A + B>();
+                else landed<B>();
+                f32x4 s[4];
+                scores<D>(s, stage + b % St::kKeys * St::kHalf, exps, q, lane);
+                read_done();
+                const uint8_t* after = next;
+                if (two_more) {
+                    after = part(b + 2);
+                    copy_keys<D>(lds, b + 2, after, lane);
+                }
+                uint32_t p[4][2];
+                weights<D>(run, p, s, a.scale_log2, limit - at, at + kBlock - 1 > len, lane);
+                if (two_more) landed<A>();
+                else landed<0>();
+                add_values<D>(run, p, stage + St::kV, exps, lane);
+                read_done();
+                if (one_more) copy_values<D>(lds, next, lane);
                 next = after;
             }
         }
-        // the four waves' results
-        run.l += __shfl_xor(run.l, 16);
-        run.l += __shfl_xor(run.l, 32);
-        __syncthreads();                                                    // the tile before has been read
-        if (quad == 0) {
-            sM[wave][c] = run.m;
-            sL[wave][c] = run.l;
-        }
+        const float l = run.l[0];
+        if (!real) continue;
+        // the lane's values: dimensions E (4 quarter + i) + j of its column, D / 4 in a row
+        if (r.part >= 0) {
+            const size_t slot = ((size_t)r.part * a.n_kv + h) * kFewCols + c;
+            float* o = a.few_acc + slot * D + quad * (D / 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < D / 16; j += 4)
-                *reinterpret_cast<f32x4*>(&sAcc[wave][c][(D / 16) * (4 * quad + i) + j]) =
-                    f32x4{run.acc[j][i], run.acc[j + 1][i], run.acc[j + 2][i], run.acc[j + 3][i]};
-        __syncthreads();
-        constexpr int V = D * kFewCols / 256;                               // values of a thread
-        const int cc = tid / 16, d0 = (tid % 16) * V;
-        if (!column(r, a.group, a.T, e.tile * kFewCols + cc, token, head)) continue;    // (no barrier behind this in the loop but the next item's first)
-        float m = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, sM[w][cc]);
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f, acc[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = exp2_fast(sM[w][cc] - base);
-            l += f * sL[w][cc];
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] += f * sAcc[w][cc][d0 + j];
-        }
-        if (e.part >= 0) {
-            const size_t slot = ((size_t)e.part * a.n_kv + h) * kFewCols + cc;
-#pragma unroll
-            for (int j = 0; j < V; ++j) a.few_acc[slot * D + d0 + j] = acc[j];
-            if (tid % 16 == 0) {
-                a.few_ml[slot * 2] = m;
+                for (int j = 0; j < D / 16; j += 4)
+                    *reinterpret_cast<f32x4*>(o + (D / 16) * i + j) = f32x4{run.acc[j][i], run.acc[j + 1][i], run.acc[j + 2][i], run.acc[j + 3][i]};
+            if (quad == 0) {
+                a.few_ml[slot * 2] = run.m;
                 a.few_ml[slot * 2 + 1] = l;
             }
         } else {
-            const float f = l == 0.f ? 0.f : 1.0f / l;                      // no key at all: a refused request, its rows are zero
-            uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + d0;
+            const float f = l == 0.f ? 0.f : 1.0f / l;              // no key at all: a refused request, its rows are zero
+            uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + quad * (D / 4);
 #pragma unroll
-            for (int j = 0; j < V; j += 2) *reinterpret_cast<uint32_t*>(o + j) = pack_bf16(acc[j] * f, acc[j + 1] * f);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < D / 16; j += 4)
+                    *reinterpret_cast<u32x2*>(o + (D / 16) * i + j) = u32x2{pack_bf16(run.acc[j][i] * f, run.acc[j + 1][i] * f),
+                                                                          pack_bf16(run.acc[j + 2][i] * f, run.acc[j + 3][i] * f)};
         }
     }
 }
@@ -330,29 +446,20 @@ template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, con
     }
 }
 
-__device__ inline float max_halves(float x)
-{
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-
-// Weights may grow to 2^kSlack times those of the running maximum before the sums are scaled down: most blocks then leave them alone.
-constexpr float kSlack = 8.f;
-
 template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
 {
     constexpr int S = D / 16, N = D / 32;
     __shared__ Tile<D> tiles[2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 31, h = lane >> 5;
     const int item = blockIdx.x;
-    if (item >= a.t.head->n_many * a.n_kv) return;
     const Entry e = a.t.many[item / a.n_kv];
+    if (e.rows == 0) return;
     const int hk = item % a.n_kv;
-    const Request r = a.t.request[e.request];
     int token, head;
-    const bool real = column(r, a.group, a.T, e.tile * kManyCols + wave * 32 + i, token, head);
-    const int limit = real ? r.len + token : -1;
+    const bool real = column(e, a.group, a.T, e.tile * kManyCols + wave * 32 + i, token, head);
+    const int limit = real ? e.len + token : -1;
     const Place pl = place();
-    const int32_t* blocks = a.t.table + (size_t)(r.held >= 0 ? r.row : 0) * a.t.row_blocks;
+    const int32_t* blocks = a.t.table + (size_t)e.row * a.t.row_blocks;
     const uint8_t* cache = a.cache + (size_t)hk * Part<D>::kBytes;
     const size_t stride = (size_t)a.n_kv * Part<D>::kBytes;
     // (a row that has been released since the plan has no block there)
@@ -360,7 +467,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 
     u32x4 q[S];
     {
-        const size_t row = min(r.first + (real ? token : 0), a.T - 1);
+        const size_t row = min(e.first + (real ? token : 0), a.T - 1);
         const uint16_t* p = a.q + row * a.q_stride + ((size_t)hk * a.group + (real ? head : 0)) * D + 8 * h;
 #pragma unroll
         for (int s = 0; s < S; ++s) q[s] = load16(p + 16 * s);
@@ -400,7 +507,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 #pragma unroll
             for (int k = 0; k < 2; ++k) s[k] *= a.scale_log2;
         }
-        if (b * kBlock + kBlock - 1 > r.len) {         // some column may not see the whole block
+        if (b * kBlock + kBlock - 1 > e.len) {         // some column may not see the whole block
             const int room = limit - b * kBlock - 4 * h;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
@@ -452,7 +559,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
         }
     } else {
         const float f = l == 0.f ? 0.f : 1.0f / l;
-        uint16_t* out = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)hk * a.group + head) * D + 4 * h;
+        uint16_t* out = a.out + (size_t)(e.first + token) * a.out_stride + ((size_t)hk * a.group + head) * D + 4 * h;
 #pragma unroll
         for (int d = 0; d < N; ++d)
 #pragma unroll
@@ -462,76 +569,72 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
     }
 }
 
-// The partial results of tiles that were cut along their keys.  D / 4 lanes take a column, four dimensions each.  Where there are many
-// pieces, a workgroup's groups of lanes share those of one column (blockIdx.y).
+// The partial results of tiles that were cut along their keys, in one pass with a running maximum.  D / 4 lanes take a column, four
+// dimensions each; the groups of lanes of a workgroup have a column each, or share the pieces of one where there are many.
 template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs a)
 {
     constexpr int L = D / 4, GROUPS = 256 / L;
-    __shared__ float sAcc[GROUPS][D], sL[GROUPS];
+    __shared__ float sAcc[GROUPS][D], sM[GROUPS], sL[GROUPS];
     const int tid = threadIdx.x, lane = tid % L, group = tid / L;
-    const int n_items = a.t.head->n_merge * a.n_kv;
-    for (int item = blockIdx.x; item < n_items; item += gridDim.x) {
+    for (int item = blockIdx.x; item < a.n_merge * a.n_kv; item += gridDim.x) {
         const Merge g = a.t.merge[item / a.n_kv];
-        const int h = item % a.n_kv, splits = abs(g.splits), cols = g.splits < 0 ? kManyCols : kFewCols;
-        const float* part_acc = g.splits < 0 ? a.many_acc : a.few_acc;
-        const float* part_ml = g.splits < 0 ? a.many_ml : a.few_ml;
-        const Request r = a.t.request[g.request];
-        const size_t slot0 = ((size_t)g.part * a.n_kv + h) * cols + g.col % cols, step = (size_t)a.n_kv * cols;
-        const bool share = splits >= 2 * GROUPS;       // (the same for the whole workgroup, like everything but `group` and `lane`)
-        if (!share && blockIdx.y) continue;
-        for (int c = share ? (int)blockIdx.y : group; c < kMergeCols; c += share ? (int)gridDim.y : GROUPS) {
+        if (g.rows == 0) return;
+        const int h = item % a.n_kv, cols = g.many ? kManyCols : kFewCols;
+        const bool share = g.cols == 1;                // (the same for the whole workgroup, like everything but `group` and `lane`)
+        for (int c = share ? 0 : group; c < g.cols; c += GROUPS) {
             int token, head;
-            if (!column(r, a.group, a.T, g.col + c, token, head)) break;
+            if (!column(g, a.group, a.T, g.col + c, token, head)) break;
+            const size_t step = (size_t)a.n_kv * cols, slot0 = ((size_t)g.part * a.n_kv + h) * cols + g.col % cols + c;
+            const float* ml = (g.many ? a.many_ml : a.few_ml) + 2 * slot0;
+            const float* p = (g.many ? a.many_acc : a.few_acc) + slot0 * D + 4 * lane;
             float m = -INFINITY, l = 0.f;
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-            const float* ml = part_ml + 2 * (slot0 + c);
-            for (int s = share ? lane : 0; s < splits; s += share ? L : 1) m = fmaxf(m, ml[2 * step * s]);
-            if (share)
-                for (int d = 1; d < L; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-            const float base = m == -INFINITY ? 0.f : m;
-            const float* p = part_acc + (slot0 + c) * D + 4 * lane;
+            auto add = [&](float m1, float l1, f32x4 x) {
+                const float grown = fmaxf(m, m1), base = grown == -INFINITY ? 0.f : grown;
+                const float f0 = exp2_fast(m - base), f1 = exp2_fast(m1 - base);
+                l = l * f0 + l1 * f1;
+                acc = acc * f0 + x * f1;
+                m = grown;
+            };
 #pragma unroll 4
-            for (int s = share ? group : 0; s < splits; s += share ? GROUPS : 1) {
-                const float f = exp2_fast(ml[2 * step * s] - base);
-                l += f * ml[2 * step * s + 1];
-                acc += f * *reinterpret_cast<const f32x4*>(p + step * D * s);
-            }
+            for (int s = share ? group : 0; s < g.splits; s += share ? GROUPS : 1)
+                add(ml[2 * step * s], ml[2 * step * s + 1], *reinterpret_cast<const f32x4*>(p + step * D * s));
             if (share) {
                 __syncthreads();
                 *reinterpret_cast<f32x4*>(&sAcc[group][4 * lane]) = acc;
-                if (lane == 0) sL[group] = l;
-                __syncthreads();
-                acc = f32x4{0.f, 0.f, 0.f, 0.f};
-                l = 0.f;
-#pragma unroll
-                for (int w = 0; w < GROUPS; ++w) {
-                    acc += *reinterpret_cast<const f32x4*>(&sAcc[w][4 * lane]);
-                    l += sL[w];
+                if (lane == 0) {
+                    sM[group] = m;
+                    sL[group] = l;
                 }
+                __syncthreads();
                 if (group) continue;
+#pragma unroll
+                for (int w = 1; w < GROUPS; ++w) add(sM[w], sL[w], *reinterpret_cast<const f32x4*>(&sAcc[w][4 * lane]));
             }
             const float f = l == 0.f ? 0.f : 1.0f / l;
-            uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + 4 * lane;
+            uint16_t* o = a.out + (size_t)(g.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + 4 * lane;
             *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16(acc[0] * f, acc[1] * f), pack_bf16(acc[2] * f, acc[3] * f)};
         }
     }
 }
 
-template <int D> hipError_t attend(const AttendArgs& a, int n_cus, long most_few, long most_many, hipStream_t stream)
+template <int D> hipError_t attend(const AttendArgs& a, int n, int n_cus, hipStream_t stream)
 {
-    if (most_many > 0) attend_many_kernel<D><<<(unsigned)(most_many * a.n_kv), 256, 0, stream>>>(a);
-    const int grid = (int)std::max<long>(1, std::min<long>(most_few * a.n_kv, 3L * n_cus));
-    attend_few_kernel<D><<<grid, 256, 0, stream>>>(a);
-    merge_kernel<D><<<dim3(4 * n_cus, 4), 256, 0, stream>>>(a);
+    if (a.n_many > 0) attend_many_kernel<D><<<(unsigned)a.n_many * a.n_kv, 256, 0, stream>>>(a);
+    // a workgroup per piece: which of them end early is for the hardware to fill (apart from refused requests a request has kFewMost
+    // columns at most; more pieces than that go round)
+    const long few = std::min<long>(a.n_few, (long)n * (kFewMost / kFewCols) + kFewItems / a.n_kv + 1);
+    attend_few_kernel<D><<<(unsigned)std::min<long>(few * a.n_kv, 1 << 20), 64, 0, stream>>>(a);
+    merge_kernel<D><<<(unsigned)std::min<long>((long)a.n_merge * a.n_kv, 4L * n_cus), 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_attend(const AttendArgs& a, int dim, int n_cus, long most_few, long most_many, hipStream_t stream)
+hipError_t launch_attend(const AttendArgs& a, int dim, int n, int n_cus, hipStream_t stream)
 {
     if (a.T == 0) return hipSuccess;
-    return dim == 64 ? attend<64>(a, n_cus, most_few, most_many, stream) : attend<128>(a, n_cus, most_few, most_many, stream);
+    return dim == 64 ? attend<64>(a, n, n_cus, stream) : attend<128>(a, n, n_cus, stream);
 }
 
 }  // namespace kv

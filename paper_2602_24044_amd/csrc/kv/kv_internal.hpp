@@ -73,22 +73,32 @@ struct Request {
     int32_t pad_[2];
 };
 
-// A piece of a step's attention: a tile of columns against a range of blocks, for every key head.
+// A piece of a step's attention: a tile of columns against a range of blocks, for every key head.  It has with it what a kernel would
+// otherwise fetch one after the other from the request and the block table (a piece is short: that chain of round trips would be a good
+// part of it).
+constexpr int kEntryIds = 8;
 struct Entry {
-    int32_t request;
+    int32_t first;     // token row of the step that the request starts at
+    int32_t rows;      // its token rows; 0: the list has ended (every entry behind the last one says so)
+    int32_t len;       // its tokens cached before the step
     int32_t tile;
     int32_t block;     // first block of the range
     int32_t blocks;    // 0: nothing to read, the rows are set to zero
     int32_t part;      // partial result that it writes, -1: the output itself
-    int32_t pad_[3];
+    int32_t row;       // row of the block table
+    uint32_t id[kEntryIds];   // the range's first blocks in the cache
 };
-// Columns whose tile's range was split: the partial results are merged behind.
-constexpr int kMergeCols = 8;
+static_assert(sizeof(Entry) == 64, "one line");
+// Columns whose tile's range was split: the partial results are merged behind.  kMergeCols columns an entry, or one where there are at least
+// kMergeMany pieces (all lanes of a workgroup then work on it).
+constexpr int kMergeCols = 8, kMergeMany = 16;
 struct Merge {
-    int32_t request;
-    int32_t col;       // first of kMergeCols columns
+    int32_t first, rows;   // as in Entry
+    int32_t col, cols; // first column, and how many
     int32_t part;      // first partial result of their tile
-    int32_t splits;    // negative: a tile of kManyCols columns
+    int32_t splits;
+    int32_t many;      // a tile of kManyCols columns
+    int32_t pad_;
 };
 
 struct Header {
@@ -159,14 +169,15 @@ struct AttendArgs {
     float *many_acc, *many_ml;          // likewise with kManyCols
     float scale_log2;                   // scale * log2(e)
     int32_t T, n_kv, group;
+    int32_t n_few, n_many, n_merge;     // entries that the lists can have (n_many 0: none)
 };
 
 hipError_t launch_plan(const PlanArgs& a, hipStream_t stream);
 hipError_t launch_release(const Tables& t, int n, const int32_t* seq, const int32_t* keep, hipStream_t stream);
 hipError_t launch_heads(const HeadsArgs& a, int dim, hipStream_t stream);
 hipError_t launch_read(const ReadArgs& a, int dim, hipStream_t stream);
-// most_few, most_many: entries that the lists can have
-hipError_t launch_attend(const AttendArgs& a, int dim, int n_cus, long most_few, long most_many, hipStream_t stream);
+// n: requests of the step
+hipError_t launch_attend(const AttendArgs& a, int dim, int n, int n_cus, hipStream_t stream);
 
 }  // namespace kv
 }  // namespace lora

@@ -190,7 +190,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
             v[1] = q.many ? pieces : 0;
             v[2] = q.splits > 1 ? v[0] : 0;
             v[3] = q.splits > 1 ? v[1] : 0;
-            v[4] = q.splits > 1 ? (q.rows * a.group + kMergeCols - 1) / kMergeCols : 0;
+            const int together = q.splits < kMergeMany ? kMergeCols : 1;
+            v[4] = q.splits > 1 ? (q.rows * a.group + together - 1) / together : 0;
         }
         scan<5>(v, total, sums);
         if (i < n) {
@@ -202,6 +203,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
 #pragma unroll
         for (int k = 0; k < 5; ++k) at[k] += total[k];
     }
+    // what the lists of the step before had behind these
+    for (int k = at[0] + tid; k < t.head->n_few; k += kPlanThreads) t.few[k].rows = 0;
+    for (int k = at[1] + tid; k < t.head->n_many; k += kPlanThreads) t.many[k].rows = 0;
+    for (int k = at[4] + tid; k < t.head->n_merge; k += kPlanThreads) t.merge[k].rows = 0;
+    __syncthreads();
     if (tid == 0) {
         t.head->n_few = at[0];
         t.head->n_many = at[1];
@@ -238,7 +244,10 @@ __global__ __launch_bounds__(256) void fill_kernel(PlanArgs a)
     Entry* list = q.many ? t.many : t.few;
     for (int k = threadIdx.x; k < q.tiles * q.splits; k += 256) {
         Entry e = {};
-        e.request = blockIdx.x;
+        e.first = q.first;
+        e.rows = q.rows;
+        e.len = q.len;
+        e.row = q.held >= 0 ? q.row : 0;
         e.tile = q.tiles - 1 - k / q.splits;
         e.block = (k % q.splits) * q.chunk;
         // the last token of the tile sees this many blocks
@@ -246,12 +255,17 @@ __global__ __launch_bounds__(256) void fill_kernel(PlanArgs a)
         const int seen = q.held >= 0 ? (q.len + last) / kBlock + 1 : 0;
         e.blocks = max(0, min(q.chunk, seen - e.block));
         e.part = q.splits > 1 ? q.part + k : -1;
+        for (int j = 0; j < min(e.blocks, kEntryIds); ++j) {
+            const int b = e.block + j;
+            e.id[j] = b < q.held ? row[b] : t.fresh[q.fresh + b - q.held];
+        }
         list[q.entry + k] = e;
     }
+    const int together = q.splits < kMergeMany ? kMergeCols : 1;
     if (q.splits > 1)
-        for (int k = threadIdx.x; k * kMergeCols < q.rows * a.group; k += 256) {
-            const int place = q.tiles - 1 - k * kMergeCols / cols;
-            t.merge[q.merge + k] = Merge{(int)blockIdx.x, k * kMergeCols, q.part + place * q.splits, q.many ? -q.splits : q.splits};
+        for (int k = threadIdx.x; k * together < q.rows * a.group; k += 256) {
+            const int place = q.tiles - 1 - k * together / cols;
+            t.merge[q.merge + k] = Merge{q.first, q.rows, k * together, together, q.part + place * q.splits, q.splits, q.many, 0};
         }
 }
 
