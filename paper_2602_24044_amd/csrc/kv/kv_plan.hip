@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
             q = t.request[i];
             const int blocks = q.held >= 0 ? (q.len + q.rows + kBlock - 1) / kBlock : 0;
             const int chunk = q.many ? chunk1 : chunk0;
-            q.splits = max(1, (blocks + chunk / 2) / chunk);
+            q.splits = max(1, (blocks + (q.many ? chunk / 2 : chunk - 1)) / chunk);
             q.chunk = (blocks + q.splits - 1) / q.splits;
             const int pieces = q.tiles * q.splits;
             v[0] = q.many ? 0 : pieces;
