@@ -126,28 +126,31 @@ __device__ inline i32x8 four_dwords(u32x4 v)
     return r;                                          // (four-bit operands are the first half)
 }
 
-// row: the column's query.
-template <int D> __device__ inline void split_query(Query<D>& q, const uint16_t* row, int lane)
+__device__ inline float positive(float scale_log2) { return scale_log2 == 0.f ? 1.f : __builtin_fabsf(scale_log2); }
+
+// The two numbers of N * 16 values of a column (their runs at p + at(j)): hi and lo, four to a dword; returns n.  The column's other
+// values are in lanes that largest() goes over.  The scale of the scores comes in here by its sign: it is positive from here on.
+template <int N, typename At, typename Largest>
+__device__ inline int split_values(int (&hi)[4 * N], int (&lo)[4 * N], const uint16_t* p, float scale_log2, At&& run, Largest&& largest)
 {
-    constexpr int H = D / 64;                          // 16 dimensions, twice with heads of 128
-    const int quad = lane >> 4;
-    u32x4 raw[2 * H];
+    u32x4 raw[2 * N];
 #pragma unroll
-    for (int j = 0; j < 2 * H; ++j) raw[j] = load16(row + 64 * (j / 2) + 16 * quad + 8 * (j % 2));
+    for (int j = 0; j < 2 * N; ++j) raw[j] = load16(p + run(j / 2) + 8 * (j % 2));
     float top = 0.f, odd = 0.f;                        // odd: a NaN where a value is a NaN or an infinity, which makes the column one
 #pragma unroll
-    for (int j = 0; j < 2 * H; ++j)
+    for (int j = 0; j < 2 * N; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float x = __builtin_fabsf(lo_f32(raw[j][i])), y = __builtin_fabsf(hi_f32(raw[j][i]));
             odd = __builtin_fmaf(x, 0.f, __builtin_fmaf(y, 0.f, odd));
             top = fmaxf(top, fmaxf(x, y));
         }
-    top = max_quarters(top);
+    top = largest(top);
     const int n = max((int)(__builtin_bit_cast(uint32_t, top) >> 23) - 127 - 7, -120);
-    const float down = __builtin_bit_cast(float, (uint32_t)(127 - n) << 23);
+    const float power = __builtin_bit_cast(float, (uint32_t)(127 - n) << 23);
+    const float down = scale_log2 > 0.f ? power : scale_log2 < 0.f ? -power : 0.f;
 #pragma unroll
-    for (int j = 0; j < 2 * H; ++j)
+    for (int j = 0; j < 2 * N; ++j)
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
             const float y[4] = {__builtin_fmaf(lo_f32(raw[j][i]), down, odd), __builtin_fmaf(hi_f32(raw[j][i]), down, odd),
@@ -157,10 +160,25 @@ template <int D> __device__ inline void split_query(Query<D>& q, const uint16_t*
             const f32x2 a0 = __builtin_amdgcn_cvt_pk_f32_fp8(a, false), a1 = __builtin_amdgcn_cvt_pk_f32_fp8(a, true);
             int b = __builtin_amdgcn_cvt_pk_fp8_f32((y[0] - a0[0]) * 16.f, (y[1] - a0[1]) * 16.f, 0, false);
             b = __builtin_amdgcn_cvt_pk_fp8_f32((y[2] - a1[0]) * 16.f, (y[3] - a1[1]) * 16.f, b, true);
-            q.x[0][2 * j + i / 2] = a;
-            if constexpr (D == 128) q.x[1][2 * j + i / 2] = b;
-            else q.x[0][4 + 2 * j + i / 2] = b;
+            hi[2 * j + i / 2] = a;
+            lo[2 * j + i / 2] = b;
         }
+    return n;
+}
+
+// row: the column's query.
+template <int D> __device__ inline void split_query(Query<D>& q, const uint16_t* row, float scale_log2, int lane)
+{
+    constexpr int N = D / 64;                          // 16 dimensions, twice with heads of 128
+    const int quad = lane >> 4;
+    int hi[4 * N], lo[4 * N];
+    const int n = split_values<N>(hi, lo, row, scale_log2, [&](int j) { return 64 * j + 16 * quad; }, [](float x) { return max_quarters(x); });
+#pragma unroll
+    for (int j = 0; j < 4 * N; ++j) {
+        q.x[0][j] = hi[j];
+        if constexpr (D == 128) q.x[1][j] = lo[j];
+        else q.x[0][4 + j] = lo[j];
+    }
     q.e[0] = n + 127 - (D == 64 && quad >= 2 ? 4 : 0);
     if constexpr (D == 128) q.e[1] = n + 127 - 4;
 }
@@ -188,16 +206,10 @@ template <int D> __device__ inline void scores(f32x4 (&s)[4], const uint8_t* key
 
 // Weights of a block's scores; limit: the last key position of the lane's column, relative to the block's first; masked: some column does
 // not see the whole block.
-template <int D> __device__ inline void weights(Running<D>& r, uint32_t (&p)[4][2], f32x4 (&s)[4], float scale_log2, int limit, bool masked, int lane)
+template <int D> __device__ inline void weights(Running<D>& r, uint32_t (&p)[4][2], f32x4 (&s)[4], float scale, int limit, bool masked, int lane)
 {
     const int quad = lane >> 4;
     float top = -INFINITY;
-    // (a positive scale is applied in the exponent below; it keeps the order of the scores)
-    if (scale_log2 <= 0.f) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) s[t] *= scale_log2;
-    }
-    const float scale = scale_log2 > 0.f ? scale_log2 : 1.f;
     if (masked)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -281,6 +293,19 @@ template <typename Of> __device__ inline bool column(const Of& r, int group, int
     return token < r.rows && r.first + token < T;
 }
 
+// Where the blocks of a piece are in the cache: 64 numbers at a time, one per lane; those behind the ones that came with the entry are
+// fetched when the first of them is asked for, which is in order.
+struct Numbers {
+    uint32_t ids;
+    __device__ Numbers(const Entry& e, int lane) : ids(e.id[lane & (kEntryIds - 1)]) {}
+    // block b of the n of the piece, which blocks[] has in the table.  (A row that has been released since the plan has none: any will do.)
+    __device__ uint32_t at(int b, const int32_t* blocks, int n, int n_blocks, int lane)
+    {
+        if (b == kEntryIds || (b && b % 64 == 0)) ids = min((unsigned)blocks[min((b & ~63) + lane, n - 1)], (unsigned)n_blocks - 1);
+        return __builtin_amdgcn_readlane(ids, b & 63);
+    }
+};
+
 template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(AttendArgs a)
 {
     using St = Stage<D>;
@@ -288,6 +313,7 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
     __shared__ __align__(1024) uint8_t stage[St::kBytes];
     const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)stage;
     const int lane = threadIdx.x, c = lane & 15, quad = lane >> 4;
+    const float scale = positive(a.scale_log2);
     for (int item = blockIdx.x; item < a.n_few * a.n_kv; item += gridDim.x) {
         const Entry& r = a.t.few[item / a.n_kv];
         if (r.rows == 0) return;
@@ -303,15 +329,8 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) run.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (n > 0) {
-            // 64 block numbers at a time, one per lane; behind those that came with the entry they are fetched meanwhile.  (A row that has
-            // been released since the plan has none: any block will do.)
-            uint32_t ids = r.id[lane & (kEntryIds - 1)];
-            auto part = [&](int b) {
-                if (b == kEntryIds || (b && b % 64 == 0))
-                    ids = min((unsigned)blocks[min((b & ~63) + lane, n - 1)], (unsigned)a.t.n_blocks - 1);
-                const uint32_t at = __builtin_amdgcn_readlane(ids, b & 63);
-                return a.cache + ((size_t)at * a.n_kv + h) * Part<D>::kBytes;
-            };
+            Numbers numbers(r, lane);
+            auto part = [&](int b) { return a.cache + ((size_t)numbers.at(b, blocks, n, a.t.n_blocks, lane) * a.n_kv + h) * Part<D>::kBytes; };
             const uint8_t *now = part(0), *next = now;
             copy_keys<D>(lds, 0, now, lane);
             if (n > 1) {
@@ -320,7 +339,7 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
             }
             copy_values<D>(lds, now, lane);
             Query<D> q;
-            split_query<D>(q, a.q + (size_t)min(r.first + (real ? token : 0), a.T - 1) * a.q_stride + ((size_t)h * a.group + (real ? head : 0)) * D, lane);
+            split_query<D>(q, a.q + (size_t)min(r.first + (real ? token : 0), a.T - 1) * a.q_stride + ((size_t)h * a.group + (real ? head : 0)) * D, a.scale_log2, lane);
             for (int b = 0; b < n; ++b) {
                 const bool one_more = b + 1 < n, two_more = b + 2 < n;
                 const int at = (first + b) * kBlock;
@@ -336,7 +355,7 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
                     copy_keys<D>(lds, b + 2, after, lane);
                 }
                 uint32_t p[4][2];
-                weights<D>(run, p, s, a.scale_log2, limit - at, at + kBlock - 1 > len, lane);
+                weights<D>(run, p, s, scale, limit - at, at + kBlock - 1 > len, lane);
                 if (two_more) landed<A>();
                 else landed<0>();
                 add_values<D>(run, p, stage + St::kV, exps, lane);
@@ -374,56 +393,50 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 }
 
 // ---- tiles of many columns ----
-// A workgroup's codes of a block of 64 keys, as its 256 threads load them: K: key tid / 4, a quarter of its dimensions; V: two
-// chunks of four keys (those that a lane of the second product wants together), kE dimensions, of which the thread converts half.
+// Four waves of 32 columns each on 32x32 MFMAs.  A block's keys are copied to LDS as they are (four-bit operands); its values go through
+// registers, where each thread converts an eighth of 16 tokens to bf16 operands of V^T in LDS, once for all four waves.  Two stages: the next
+// block is made while this one is used.
+//
+// Values, as the 256 threads load them: two chunks of four tokens (those that a lane of the second product wants together), kE dimensions,
+// of which the thread converts half.
 template <int D> struct Raw {
-    uint32_t k[D / 32], v[2][D / 32], ke, ve[2];
+    uint32_t v[2][D / 32], e[2];
 };
-
 struct Place {
-    int key, quarter;          // K
-    int u, h, half, m;         // V: keys 16 u + 4 h .. + 3 and 16 u + 8 + 4 h .. + 3, dimensions kE m .. 
+    int u, h, half, m;         // tokens 16 u + 4 h .. + 3 and 16 u + 8 + 4 h .. + 3, dimensions kE m ..
 };
 __device__ inline Place place()
 {
     const int t = threadIdx.x;
-    return Place{t >> 2, t & 3, t >> 6, (t >> 5) & 1, (t >> 4) & 1, t & 15};
+    return Place{t >> 6, (t >> 5) & 1, (t >> 4) & 1, t & 15};
 }
 
-template <int D> __device__ inline void load_raw(Raw<D>& r, const uint8_t* part, const Place& p)
+template <int D> __device__ inline void load_values(Raw<D>& r, const uint8_t* part, const Place& p)
 {
     using P = Part<D>;
-    load_words(r.k, part + P::kK + p.key * P::kRow + p.quarter * (D / 8));
-    r.ke = part[P::kKExp + P::k_exp_at(p.key, p.quarter * (D / 4) / kGroup)];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         load_words(r.v[c], part + P::kV + P::v_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE));
-        r.ve[c] = *reinterpret_cast<const uint32_t*>(part + P::kVExp + P::v_exp_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE / kGroup));
+        r.e[c] = *reinterpret_cast<const uint32_t*>(part + P::kVExp + P::v_exp_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE / kGroup));
     }
 }
 
-// The block in LDS: every operand of an MFMA is 64 lanes * 16 bytes, in lane order but for a permutation inside groups of eight that
-// spreads a wave's writes over the banks.  K: [key / 32][D / 16], V: [d / 32][key / 16].
+// A block in LDS.  Values: every operand of an MFMA is 64 lanes * 16 bytes, in lane order but for a permutation inside groups of eight that
+// spreads a wave's writes over the banks: [d / 32][key / 16].
 template <int D> struct Tile {
-    static constexpr int kKFrags = 2 * (D / 16), kVFrags = (D / 32) * 4;
-    u32x4 k[kKFrags * 64], v[kVFrags * 64];
-    __device__ static int k_at(int tile, int s, int h, int i) { return (tile * (D / 16) + s) * 64 + h * 32 + (i ^ (2 * (s * 16 / (D / 4)))); }
+    uint8_t k[kBlock * Part<D>::kRow], e[kBlock * Part<D>::kGroups];
+    u32x4 v[(D / 32) * 4 * 64];
     __device__ static int v_at(int dt, int u, int h, int i) { return (dt * 4 + u) * 64 + h * 32 + (i ^ (2 * ((i >> 3) & 3) + (dt & 1))); }
 };
 
 template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, const Place& p)
 {
     constexpr int E = Part<D>::kE;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-        const int d = p.quarter * (D / 4) + 8 * j;
-        t.k[Tile<D>::k_at(p.key >> 5, d >> 4, (d >> 3) & 1, p.key & 31)] = eight_bf16(r.k[j], r.ke << 23);
-    }
     u32x4 f[E / 2];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {                      // keys 2 x, 2 x + 1 of the thread's eight
+    for (int x = 0; x < 4; ++x) {                      // tokens 2 x, 2 x + 1 of the thread's eight
         const int c = x / 2, i = 2 * (x & 1);
-        const uint32_t e0 = i == 0 ? r.ve[c] << 23 : r.ve[c] << 7, e1 = i == 0 ? r.ve[c] << 15 : r.ve[c] >> 1;
+        const uint32_t e0 = i == 0 ? r.e[c] << 23 : r.e[c] << 7, e1 = i == 0 ? r.e[c] << 15 : r.e[c] >> 1;
         uint32_t a, b;
         if constexpr (D == 128) {
             a = r.v[c][i] >> (16 * p.half);
@@ -446,31 +459,48 @@ template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, con
     }
 }
 
+// A block's keys and their exponents to LDS (lds: where the tile is): 1 KB a wave, the exponents by the first.
+template <int D> __device__ inline void copy_block_keys(uint32_t lds, const uint8_t* part, int wave, int lane)
+{
+    constexpr int keys = kBlock * Part<D>::kRow, exps = kBlock * Part<D>::kGroups;
+    if (wave < keys / 1024) copy16(part + Part<D>::kK + 1024 * wave, 16 * lane, lds + 1024 * wave);
+    if (wave == keys / 1024 - 1 && 16 * lane < exps) copy16(part + Part<D>::kKExp, 16 * lane, lds + keys);
+}
+
 template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
 {
-    constexpr int S = D / 16, N = D / 32;
-    __shared__ Tile<D> tiles[2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 31, h = lane >> 5;
+    constexpr int X = D / 64, N = D / 32;
+    __shared__ __align__(1024) Tile<D> tiles[2];
+    const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)tiles;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
     const int item = blockIdx.x;
-    const Entry e = a.t.many[item / a.n_kv];
+    const Entry& e = a.t.many[item / a.n_kv];
     if (e.rows == 0) return;
     const int hk = item % a.n_kv;
     int token, head;
     const bool real = column(e, a.group, a.T, e.tile * kManyCols + wave * 32 + i, token, head);
     const int limit = real ? e.len + token : -1;
+    const int seen = e.len + (e.tile * kManyCols + wave * 32) / a.group;   // the last key that all of the wave's columns see
     const Place pl = place();
-    const int32_t* blocks = a.t.table + (size_t)e.row * a.t.row_blocks;
-    const uint8_t* cache = a.cache + (size_t)hk * Part<D>::kBytes;
-    const size_t stride = (size_t)a.n_kv * Part<D>::kBytes;
-    // (a row that has been released since the plan has no block there)
-    auto part = [&](int b) { return cache + (size_t)min((unsigned)blocks[b], (unsigned)a.t.n_blocks - 1) * stride; };
+    const int32_t* blocks = a.t.table + (size_t)e.row * a.t.row_blocks + e.block;
+    const int n = __builtin_amdgcn_readfirstlane(e.blocks), first = e.block;
+    Numbers numbers(e, lane);
 
-    u32x4 q[S];
+    // 32x32x64: lane (column, h) has eight-bit operands k = 16 h .. + 15 and 32 + 16 h .. + 15, four-bit ones k = 32 h .. + 31
+    i32x8 q[X][2];
+    int qe;
     {
         const size_t row = min(e.first + (real ? token : 0), a.T - 1);
-        const uint16_t* p = a.q + row * a.q_stride + ((size_t)hk * a.group + (real ? head : 0)) * D + 8 * h;
+        int hi[8 * X], lo[8 * X];
+        qe = 127 + split_values<2 * X>(hi, lo, a.q + row * a.q_stride + ((size_t)hk * a.group + (real ? head : 0)) * D, a.scale_log2,
+                                       [&](int j) { return 32 * j + 16 * h; }, [](float x) { return max_halves(x); });
 #pragma unroll
-        for (int s = 0; s < S; ++s) q[s] = load16(p + 16 * s);
+        for (int x = 0; x < X; ++x)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                q[x][0][j] = hi[8 * x + j];
+                q[x][1][j] = lo[8 * x + j];
+            }
     }
     f32x16 o[N];
 #pragma unroll
@@ -478,37 +508,63 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 #pragma unroll
         for (int x = 0; x < 16; ++x) o[d][x] = 0.f;
     float m = -INFINITY, l = 0.f;
-    const float scale = a.scale_log2 > 0.f ? a.scale_log2 : 1.f;
+    const float scale = positive(a.scale_log2);
 
     Raw<D> raw;
-    const int end = e.block + e.blocks;
-    if (e.blocks > 0) {
-        load_raw<D>(raw, part(e.block), pl);
-        convert<D>(tiles[0], raw, pl);
-        load_raw<D>(raw, part(min(e.block + 1, end - 1)), pl);
+    // A block's keys out of LDS, and one of the 4 X products that make its scores.
+    struct Keys {
+        i32x8 k[X][2];
+        int e[X];
+    };
+    auto read_keys = [&](Keys& f, const Tile<D>& t) {
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+            // exponents of keys i % 16, + 16, + 32, + 48: those of key i and i + 32 in bytes 0 and 2
+            f.e[x] = *reinterpret_cast<const int*>(t.e + Part<D>::k_exp_at(i & 15, 2 * x + h)) >> (i & 16 ? 8 : 0);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) f.k[x][k] = four_dwords(*reinterpret_cast<const u32x4*>(t.k + (32 * k + i) * Part<D>::kRow + 32 * x + 16 * h));
+        }
+    };
+    auto score = [&](f32x16 (&s)[2], const Keys& f, int j) {
+        const int x = j / 4, y = (j / 2) & 1;
+        if (j & 1) s[1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.k[x][1], q[x][y], s[1], 4, 0, 2, f.e[x], 0, qe - 4 * y);
+        else s[0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.k[x][0], q[x][y], s[0], 4, 0, 0, f.e[x], 0, qe - 4 * y);
+    };
+    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    // The loop is one block of scores ahead, so that the matrix units have work while the vector unit forms a block's weights: at the top of
+    // iteration b the scores of block b are there, its values and the next block's keys are in LDS (places b % 2 and (b + 1) % 2), and the
+    // next block's values are in registers or on their way.
+    f32x16 s[2];
+    auto at = [&](uint32_t id) { return a.cache + ((size_t)__builtin_amdgcn_readfirstlane(id) * a.n_kv + hk) * Part<D>::kBytes; };
+    if (n > 0) {
+        const uint32_t one = numbers.at(0, blocks, n, a.t.n_blocks, lane);
+        const uint32_t two = n > 1 ? numbers.at(1, blocks, n, a.t.n_blocks, lane) : one;
+        copy_block_keys<D>(lds, at(one), wave, lane);
+        copy_block_keys<D>(lds + (uint32_t)sizeof(Tile<D>), at(two), wave, lane);
+        load_values<D>(raw, at(one), pl);
+        convert<D>(tiles[0], raw, pl);                 // (waits for everything asked for so far)
+        load_values<D>(raw, at(two), pl);
+        __syncthreads();
+        Keys f;
+        read_keys(f, tiles[0]);
+        s[0] = s[1] = zero;
+#pragma unroll
+        for (int j = 0; j < 4 * X; ++j) score(s, f, j);
     }
-    for (int b = e.block, at = 0; b < end; ++b, at ^= 1) {
-        __syncthreads();                               // this block's tile is complete, and the other one has been read
-        if (b + 1 < end) {
-            convert<D>(tiles[at ^ 1], raw, pl);
-            load_raw<D>(raw, part(min(b + 2, end - 1)), pl);
+    for (int b = 0; b < n; ++b) {
+        __syncthreads();                               // what the comment above says holds for all waves, and the other places have been read
+        const int key0 = (first + b) * kBlock;
+        const Tile<D>&t = tiles[b & 1], &ahead = tiles[(b + 1) & 1];
+        // (in this order: the compiler waits for all requests in front of the first use of `raw`, and it should be for the ones that the
+        // iteration before has made)
+        convert<D>(tiles[(b + 1) & 1], raw, pl);
+        if (b + 2 < n) {
+            const uint32_t two = numbers.at(b + 2, blocks, n, a.t.n_blocks, lane);
+            copy_block_keys<D>(lds + (b & 1) * (uint32_t)sizeof(Tile<D>), at(two), wave, lane);
+            load_values<D>(raw, at(two), pl);
         }
-        const Tile<D>& t = tiles[at];
-        f32x16 s[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) s[k][x] = 0.f;
-#pragma unroll
-            for (int j = 0; j < S; ++j) s[k] = mfma32(as_bf16x8(t.k[Tile<D>::k_at(k, j, h, i)]), as_bf16x8(q[j]), s[k]);
-        }
-        // (a positive scale is applied in the exponent below; it keeps the order of the scores)
-        if (a.scale_log2 <= 0.f) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) s[k] *= a.scale_log2;
-        }
-        if (b * kBlock + kBlock - 1 > e.len) {         // some column may not see the whole block
-            const int room = limit - b * kBlock - 4 * h;
+        if (key0 + kBlock - 1 > seen) {                // some column does not see the whole block
+            const int room = limit - key0 - 4 * h;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -530,19 +586,44 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
             m = grown;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        u32x4 w[4];
+        // The order is pinned here: an MFMA of the next scores (of no use in the last iteration: what is in LDS then are older codes), and in
+        // its time a part of this block's weights on the vector unit; values from LDS a group of operands ahead of the MFMAs that want
+        // them.  Left to itself the compiler asks LDS for an operand right in front of each MFMA.
+        Keys keys;
+        read_keys(keys, ahead);
+        f32x16 s_next[2] = {zero, zero};
+        u32x4 w[4], f[2][N];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int j = 0; j < 4 * X; ++j) {
+            score(s_next, keys, j);
+            __builtin_amdgcn_sched_barrier(0);
+            if (j == 4 * X - 1)
 #pragma unroll
-            for (int x = 0; x < 16; x += 2) {
+                for (int d = 0; d < N; ++d) f[0][d] = t.v[Tile<D>::v_at(d, 0, h, i)];
+            constexpr int P = 32 / (4 * X);            // weights of a part
+#pragma unroll
+            for (int y = P * j; y < P * (j + 1); y += 2) {
+                const int k = y / 16, x = y % 16;
                 const float p0 = exp2_fast(__builtin_fmaf(s[k][x], scale, -base)), p1 = exp2_fast(__builtin_fmaf(s[k][x + 1], scale, -base));
                 l += p0 + p1;
                 w[2 * k + x / 8][(x % 8) / 2] = pack_bf16(p0, p1);
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < 4; ++u) {
+            if (u < 3)
 #pragma unroll
-            for (int d = 0; d < N; ++d) o[d] = mfma32(as_bf16x8(t.v[Tile<D>::v_at(d, u, h, i)]), as_bf16x8(w[u]), o[d]);
+                for (int d = 0; d < N; ++d) f[(u + 1) & 1][d] = t.v[Tile<D>::v_at(d, u + 1, h, i)];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int d = 0; d < N; ++d) o[d] = mfma32(as_bf16x8(f[u & 1][d]), as_bf16x8(w[u]), o[d]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) s[k] = s_next[k];
+        landed<0>();
     }
     l += __shfl_xor(l, 32);
     if (!real) return;
