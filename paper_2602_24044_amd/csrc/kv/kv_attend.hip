@@ -397,13 +397,13 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 // registers, where each thread converts an eighth of 16 tokens to bf16 operands of V^T in LDS, once for all four waves.  Two stages: the next
 // block is made while this one is used.
 //
-// Values, as the 256 threads load them: two chunks of four tokens (those that a lane of the second product wants together), kE dimensions,
-// of which the thread converts half.
+// Values, as the 256 threads load them: a chunk of four tokens, kE dimensions.  That is half of an operand of V^T for each of these: the
+// other half are the four tokens eight further.
 template <int D> struct Raw {
-    uint32_t v[2][D / 32], e[2];
+    uint32_t v[D / 32], e;
 };
 struct Place {
-    int u, h, half, m;         // tokens 16 u + 4 h .. + 3 and 16 u + 8 + 4 h .. + 3, dimensions kE m ..
+    int u, c, h, m;            // tokens 16 u + 8 c + 4 h .. + 3, dimensions kE m ..
 };
 __device__ inline Place place()
 {
@@ -414,11 +414,9 @@ __device__ inline Place place()
 template <int D> __device__ inline void load_values(Raw<D>& r, const uint8_t* part, const Place& p)
 {
     using P = Part<D>;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        load_words(r.v[c], part + P::kV + P::v_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE));
-        r.e[c] = *reinterpret_cast<const uint32_t*>(part + P::kVExp + P::v_exp_at(16 * p.u + 8 * c + 4 * p.h, p.m * P::kE / kGroup));
-    }
+    const int k = 16 * p.u + 8 * p.c + 4 * p.h;
+    load_words(r.v, part + P::kV + P::v_at(k, p.m * P::kE));
+    r.e = *reinterpret_cast<const uint32_t*>(part + P::kVExp + P::v_exp_at(k, p.m * P::kE / kGroup));
 }
 
 // A block in LDS.  Values: every operand of an MFMA is 64 lanes * 16 bytes, in lane order but for a permutation inside groups of eight that
@@ -432,30 +430,26 @@ template <int D> struct Tile {
 template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, const Place& p)
 {
     constexpr int E = Part<D>::kE;
-    u32x4 f[E / 2];
+    u32x2 f[E];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {                      // tokens 2 x, 2 x + 1 of the thread's eight
-        const int c = x / 2, i = 2 * (x & 1);
-        const uint32_t e0 = i == 0 ? r.e[c] << 23 : r.e[c] << 7, e1 = i == 0 ? r.e[c] << 15 : r.e[c] >> 1;
-        uint32_t a, b;
+    for (int x = 0; x < 2; ++x) {                      // tokens 2 x, 2 x + 1 of the four
+        const uint32_t e0 = x == 0 ? r.e << 23 : r.e << 7, e1 = x == 0 ? r.e << 15 : r.e >> 1;
+        const uint32_t a = D == 128 ? r.v[2 * x] : r.v[x], b = D == 128 ? r.v[2 * x + 1] : r.v[x] >> 16;
+        auto deal = [&](int d, uint32_t y, uint32_t z) {
+            f[d][x] = __builtin_amdgcn_perm(z, y, 0x05040100u);
+            f[d + 1][x] = __builtin_amdgcn_perm(z, y, 0x07060302u);
+        };
+        deal(0, two_bf16<0>(a, e0), two_bf16<0>(b, e1));
+        deal(2, two_bf16<1>(a, e0), two_bf16<1>(b, e1));
         if constexpr (D == 128) {
-            a = r.v[c][i] >> (16 * p.half);
-            b = r.v[c][i + 1] >> (16 * p.half);
-        } else {
-            a = r.v[c][i / 2] >> (8 * p.half);
-            b = a >> 16;
-        }
-#pragma unroll
-        for (int j = 0; j < E / 4; ++j) {
-            const uint32_t y = j == 0 ? two_bf16<0>(a, e0) : two_bf16<1>(a, e0), z = j == 0 ? two_bf16<0>(b, e1) : two_bf16<1>(b, e1);
-            f[2 * j][x] = __builtin_amdgcn_perm(z, y, 0x05040100u);
-            f[2 * j + 1][x] = __builtin_amdgcn_perm(z, y, 0x07060302u);
+            deal(4, two_bf16<2>(a, e0), two_bf16<2>(b, e1));
+            deal(6, two_bf16<3>(a, e0), two_bf16<3>(b, e1));
         }
     }
 #pragma unroll
-    for (int j = 0; j < E / 2; ++j) {
-        const int d = E * p.m + (E / 2) * p.half + j;
-        t.v[Tile<D>::v_at(d >> 5, p.u, p.h, d & 31)] = f[j];
+    for (int j = 0; j < E; ++j) {
+        const int d = E * p.m + j;
+        reinterpret_cast<u32x2*>(&t.v[Tile<D>::v_at(d >> 5, p.u, p.h, d & 31)])[p.c] = f[j];
     }
 }
 
@@ -551,7 +545,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 #pragma unroll
         for (int j = 0; j < 4 * X; ++j) score(s, f, j);
     }
-    for (int b = 0; b < n; ++b) {
+    auto step = [&](int b, f32x16 (&s)[2], f32x16 (&s_next)[2]) {
         __syncthreads();                               // what the comment above says holds for all waves, and the other places have been read
         const int key0 = (first + b) * kBlock;
         const Tile<D>&t = tiles[b & 1], &ahead = tiles[(b + 1) & 1];
@@ -591,7 +585,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
         // them.  Left to itself the compiler asks LDS for an operand right in front of each MFMA.
         Keys keys;
         read_keys(keys, ahead);
-        f32x16 s_next[2] = {zero, zero};
+        s_next[0] = s_next[1] = zero;
         u32x4 w[4], f[2][N];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -606,8 +600,9 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
             for (int y = P * j; y < P * (j + 1); y += 2) {
                 const int k = y / 16, x = y % 16;
                 const float p0 = exp2_fast(__builtin_fmaf(s[k][x], scale, -base)), p1 = exp2_fast(__builtin_fmaf(s[k][x + 1], scale, -base));
-                l += p0 + p1;
-                w[2 * k + x / 8][(x % 8) / 2] = pack_bf16(p0, p1);
+                const uint32_t two = pack_bf16(p0, p1);
+                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+                w[2 * k + x / 8][(x % 8) / 2] = two;
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -621,9 +616,12 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
             for (int d = 0; d < N; ++d) o[d] = mfma32(as_bf16x8(f[u & 1][d]), as_bf16x8(w[u]), o[d]);
             __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) s[k] = s_next[k];
         landed<0>();
+    };
+    f32x16 s_other[2];
+    for (int b = 0; b < n; b += 2) {                   // (two steps, whose scores change places without being moved)
+        step(b, s, s_other);
+        if (b + 1 < n) step(b + 1, s_other, s);
     }
     l += __shfl_xor(l, 32);
     if (!real) return;
