@@ -61,11 +61,23 @@ template <int D> struct Stage {
     static constexpr int kV = kKeys * kHalf, kE = kV + kHalf, kBytes = kE + kExpPlaces * kExps;
 };
 
-// 16 bytes per active lane, lane * 16 behind `from`, to LDS at lds + 16 * lane.  m0 carries the LDS address (the compiler writes it itself
-// directly in front of its own uses); the copy wants a wait state behind the write.
-__device__ inline void copy16(const uint8_t* from, uint32_t lane16, uint32_t lds)
+// Keys in LDS: a row of codes per key as in the cache, but for the 16-byte pieces of a row, which change places (by the bits of the key above
+// those that 256 bytes hold) so that lanes that read the same piece of neighbouring keys meet different banks.  A copy writes LDS in
+// lane order, so it is the lanes' addresses in memory that are dealt out; keys 16 (32 with heads of 64) apart are alike.
+template <int D> __device__ inline int key_at(int k, int piece)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(lane16), "s"(from), "s"(lds) : "memory");
+    return k * Part<D>::kRow + 16 * (piece ^ (D == 128 ? (k >> 2) & 3 : (k >> 3) & 1));
+}
+template <int D> __device__ inline uint32_t key_from(int lane)
+{
+    return 16 * (lane ^ (D == 128 ? lane >> 4 : (lane >> 4) & 1));
+}
+
+// 16 bytes per active lane, `offset` behind `from`, to LDS at lds + 16 * lane.  m0 carries the LDS address (the compiler writes it itself
+// directly in front of its own uses); the copy wants a wait state behind the write.
+__device__ inline void copy16(const uint8_t* from, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(lds) : "memory");
 }
 // All but the wave's latest N requests to memory have come back.
 template <int N> __device__ inline void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
@@ -78,7 +90,7 @@ template <int D> __device__ inline void copy_keys(uint32_t lds, int b, const uin
     using T = Stage<D>;
     if (16 * lane < T::kExps) copy16(part + Part<D>::kKExp, 16 * lane, lds + T::kE + b % T::kExpPlaces * T::kExps);
 #pragma unroll
-    for (int c = 0; c < T::kCopies; ++c) copy16(part + Part<D>::kK + 1024 * c, 16 * lane, lds + b % T::kKeys * T::kHalf + 1024 * c);
+    for (int c = 0; c < T::kCopies; ++c) copy16(part + Part<D>::kK + 1024 * c, key_from<D>(lane), lds + b % T::kKeys * T::kHalf + 1024 * c);
 }
 template <int D> __device__ inline void copy_values(uint32_t lds, const uint8_t* part, int lane)
 {
@@ -191,7 +203,7 @@ template <int D> __device__ inline void scores(f32x4 (&s)[4], const uint8_t* key
     i32x8 k[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        k[t] = four_dwords(*reinterpret_cast<const u32x4*>(keys + (16 * t + m) * Part<D>::kRow + 16 * g));
+        k[t] = four_dwords(*reinterpret_cast<const u32x4*>(keys + key_at<D>(16 * t + m, g)));
         s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // (formats: 4 = e2m1, 0 = e4m3; the number behind is the byte of the exponents)
@@ -419,12 +431,12 @@ template <int D> __device__ inline void load_values(Raw<D>& r, const uint8_t* pa
     r.e = *reinterpret_cast<const uint32_t*>(part + P::kVExp + P::v_exp_at(k, p.m * P::kE / kGroup));
 }
 
-// A block in LDS.  Values: every operand of an MFMA is 64 lanes * 16 bytes, in lane order but for a permutation inside groups of eight that
-// spreads a wave's writes over the banks: [d / 32][key / 16].
+// A block in LDS.  Values: every operand of an MFMA is 64 lanes * 16 bytes, in lane order but for a permutation inside groups of four that
+// spreads a wave's writes over the banks: [d / 32][key / 16].  (Reads take lanes four by four, not all of them neighbours.)
 template <int D> struct Tile {
     uint8_t k[kBlock * Part<D>::kRow], e[kBlock * Part<D>::kGroups];
     u32x4 v[(D / 32) * 4 * 64];
-    __device__ static int v_at(int dt, int u, int h, int i) { return (dt * 4 + u) * 64 + h * 32 + (i ^ (2 * ((i >> 3) & 3) + (dt & 1))); }
+    __device__ static int v_at(int dt, int u, int h, int i) { return (dt * 4 + u) * 64 + h * 32 + (i ^ (2 * ((i >> 4) & 1) + (dt & 1))); }
 };
 
 template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, const Place& p)
@@ -457,7 +469,7 @@ template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, con
 template <int D> __device__ inline void copy_block_keys(uint32_t lds, const uint8_t* part, int wave, int lane)
 {
     constexpr int keys = kBlock * Part<D>::kRow, exps = kBlock * Part<D>::kGroups;
-    if (wave < keys / 1024) copy16(part + Part<D>::kK + 1024 * wave, 16 * lane, lds + 1024 * wave);
+    if (wave < keys / 1024) copy16(part + Part<D>::kK + 1024 * wave, key_from<D>(lane), lds + 1024 * wave);
     if (wave == keys / 1024 - 1 && 16 * lane < exps) copy16(part + Part<D>::kKExp, 16 * lane, lds + keys);
 }
 
@@ -516,7 +528,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
             // exponents of keys i % 16, + 16, + 32, + 48: those of key i and i + 32 in bytes 0 and 2
             f.e[x] = *reinterpret_cast<const int*>(t.e + Part<D>::k_exp_at(i & 15, 2 * x + h)) >> (i & 16 ? 8 : 0);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) f.k[x][k] = four_dwords(*reinterpret_cast<const u32x4*>(t.k + (32 * k + i) * Part<D>::kRow + 32 * x + 16 * h));
+            for (int k = 0; k < 2; ++k) f.k[x][k] = four_dwords(*reinterpret_cast<const u32x4*>(t.k + key_at<D>(32 * k + i, 2 * x + h)));
         }
     };
     auto score = [&](f32x16 (&s)[2], const Keys& f, int j) {
