@@ -516,36 +516,45 @@ def lora_kv_destroy(kv: int) -> None:
     _kv_check(_lib.lora_kv_destroy(_P(kv)), "lora_kv_destroy")
 
 
+# (Addresses go through as integers: the argument types make pointers of them.)
 def lora_kv_extend(kv: int, n: int, d_seq: int, d_len: int, d_new: int, T: int, max_new: int, stream: int = 0) -> lora_kv_step:
     step = lora_kv_step()
-    _kv_check(_lib.lora_kv_extend(_P(kv), int(n), _P(d_seq or None), _P(d_len or None), _P(d_new or None), int(T),
-                                  int(max_new), ctypes.byref(step), _P(stream or None)), "lora_kv_extend")
+    st = _lib.lora_kv_extend(kv, n, d_seq or None, d_len or None, d_new or None, T, max_new, step, stream or None)
+    if st != LORA_OK:
+        raise LoraError(st, "lora_kv_extend")
     return step
 
 
 def lora_kv_release(kv: int, n: int, d_seq: int, d_keep: int = 0, stream: int = 0) -> None:
-    _kv_check(_lib.lora_kv_release(_P(kv), int(n), _P(d_seq or None), _P(d_keep or None), _P(stream or None)), "lora_kv_release")
+    st = _lib.lora_kv_release(kv, n, d_seq or None, d_keep or None, stream or None)
+    if st != LORA_OK:
+        raise LoraError(st, "lora_kv_release")
 
 
 def lora_head_norm_rotate(T: int, n_heads: int, n_kv_heads: int, head_dim: int, d_position: int, heads: lora_heads,
                           stream: int = 0) -> None:
-    _kv_check(_lib.lora_head_norm_rotate(int(T), int(n_heads), int(n_kv_heads), int(head_dim), _P(d_position or None),
-                                         ctypes.byref(heads), _P(stream or None)), "lora_head_norm_rotate")
+    st = _lib.lora_head_norm_rotate(T, n_heads, n_kv_heads, head_dim, d_position or None, heads, stream or None)
+    if st != LORA_OK:
+        raise LoraError(st, "lora_head_norm_rotate")
 
 
 def lora_kv_store(kv: int, layer: int, step: lora_kv_step, heads: lora_heads, stream: int = 0) -> None:
-    _kv_check(_lib.lora_kv_store(_P(kv), int(layer), ctypes.byref(step), ctypes.byref(heads), _P(stream or None)), "lora_kv_store")
+    st = _lib.lora_kv_store(kv, layer, step, heads, stream or None)
+    if st != LORA_OK:
+        raise LoraError(st, "lora_kv_store")
 
 
 def lora_kv_attend(kv: int, layer: int, step: lora_kv_step, scale: float, d_q: int, d_out: int, q_stride: int = 0,
                    out_stride: int = 0, stream: int = 0) -> None:
-    _kv_check(_lib.lora_kv_attend(_P(kv), int(layer), ctypes.byref(step), float(scale), _P(d_q or None), int(q_stride),
-                                  _P(d_out or None), int(out_stride), _P(stream or None)), "lora_kv_attend")
+    st = _lib.lora_kv_attend(kv, layer, step, scale, d_q or None, q_stride, d_out or None, out_stride, stream or None)
+    if st != LORA_OK:
+        raise LoraError(st, "lora_kv_attend")
 
 
 def lora_kv_read(kv: int, layer: int, n: int, d_seq: int, d_position: int, d_k_out: int, d_v_out: int, stream: int = 0) -> None:
-    _kv_check(_lib.lora_kv_read(_P(kv), int(layer), int(n), _P(d_seq or None), _P(d_position or None), _P(d_k_out or None),
-                                _P(d_v_out or None), _P(stream or None)), "lora_kv_read")
+    st = _lib.lora_kv_read(kv, layer, n, d_seq or None, d_position or None, d_k_out or None, d_v_out or None, stream or None)
+    if st != LORA_OK:
+        raise LoraError(st, "lora_kv_read")
 
 
 def lora_kv_poll_flags(kv: int, stream: int = 0) -> Tuple[int, int]:

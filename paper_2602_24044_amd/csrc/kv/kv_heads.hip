@@ -10,6 +10,8 @@
 // throughout and rounded to 32 once: next to a border between two codes an error of 2^-24 would pick the wrong one now and then.
 #include "kv_device.hpp"
 
+#include <type_traits>
+
 namespace lora {
 namespace kv {
 namespace {
@@ -49,52 +51,109 @@ __device__ inline void sin_cos(double a, double& s, double& c)
 }
 
 
-// One row of D values: R = float (queries) or double (keys).
-template <int D, typename R>
-__device__ inline void norm_rotate(const u32x4 raw, const uint16_t* weight, float eps, const double2* cs, bool rotate, bool pairs, R (&y)[8])
+// Over the L lanes of a row: the value of the lane L / 2 away, and the sum.  With 16 lanes a row is one of the vector unit's.
+template <int L, typename T> __device__ inline T across(T v)
+{
+    static_assert(sizeof(T) == 4, "");
+    if constexpr (L == 16) return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
+    else return __shfl_xor(v, L / 2);
+}
+template <int L> __device__ inline float row_sum(float v)
+{
+    if constexpr (L == 16) {
+        auto turn = [](float x, auto by) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(by)::value, 0xf, 0xf, true)); };
+        v += turn(v, std::integral_constant<int, 0x128>());
+        v += turn(v, std::integral_constant<int, 0x124>());
+        v += turn(v, std::integral_constant<int, 0x122>());
+        return v + turn(v, std::integral_constant<int, 0x121>());
+    } else {
+#pragma unroll
+        for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d);
+        return v;
+    }
+}
+template <int L> __device__ inline double row_sum(double v)
+{
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// What a lane needs for every row of a token: cos and sin of its pairs, and with a norm the weights of its values and of those of the lane that
+// has their partners.  R = float (queries, and keys that stay bf16) or double (keys on their way to four bits).
+template <int D, typename R> struct Turn {
+    R c[8], s[8];
+};
+template <typename R> struct Weights {
+    bool on;
+    R own[8], other[8];
+};
+template <int D, typename R> __device__ inline void load_weights(Weights<R>& w, const uint16_t* p)
 {
     constexpr int L = D / 8;
     const int l = threadIdx.x % L;
-    R x[8];
+    w.on = p != nullptr;
+    if (!w.on) return;
+    const u32x4 a = load16(p + 8 * l), b = load16(p + 8 * (l ^ (L / 2)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        w.own[2 * j] = (R)lo_f32(a[j]);
+        w.own[2 * j + 1] = (R)hi_f32(a[j]);
+        w.other[2 * j] = (R)lo_f32(b[j]);
+        w.other[2 * j + 1] = (R)hi_f32(b[j]);
+    }
+}
+template <int D, typename R> __device__ inline void load_turn(Turn<D, R>& t, const double2* cs, bool pairs)
+{
+    const int l = threadIdx.x % (D / 8);
+    // halves: pair p = (8 l + j) % (D / 2), and the second half takes the sine with its own sign; neighbours: pair 4 l + j / 2
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const double2 v = cs[pairs ? 4 * l + j / 2 : (8 * l + j) % (D / 2)];
+        t.c[j] = (R)v.x;
+        t.s[j] = (R)((pairs ? (j & 1) : l >= D / 16) ? v.y : -v.y);
+    }
+}
+
+// Norm and rotation of one row of D values, eight of them in a lane.
+template <int D, typename R>
+__device__ inline void norm_rotate(const u32x4 raw, const Weights<R>& w, float eps, const Turn<D, R>& t, bool rotate, bool pairs, R (&y)[8])
+{
+    constexpr int L = D / 8;
+    R x[8], inv = 1;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         x[2 * j] = (R)lo_f32(raw[j]);
         x[2 * j + 1] = (R)hi_f32(raw[j]);
     }
-    if (weight) {
+    if (w.on) {
         R sum = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
-#pragma unroll
-        for (int d = 1; d < L; d <<= 1) sum += __shfl_xor(sum, d);
-        const R mean = sum / (R)D + (R)eps;
-        R inv;
+        const R mean = row_sum<L>(sum) / (R)D + (R)eps;
         if constexpr (sizeof(R) == 8) inv = 1.0 / __builtin_sqrt(mean);
         else inv = 1.0f / __builtin_sqrtf(mean);
-        const u32x4 w = load16(weight + 8 * l);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[2 * j] *= inv * (R)lo_f32(w[j]);
-            x[2 * j + 1] *= inv * (R)hi_f32(w[j]);
-        }
+        for (int j = 0; j < 8; ++j) x[j] *= inv * w.own[j];
     }
     if (!rotate) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = x[j];
     } else if (pairs) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const double2 t = cs[4 * l + j];
-            y[2 * j] = x[2 * j] * (R)t.x - x[2 * j + 1] * (R)t.y;
-            y[2 * j + 1] = x[2 * j + 1] * (R)t.x + x[2 * j] * (R)t.y;
-        }
+        for (int j = 0; j < 8; ++j) y[j] = x[j] * t.c[j] + x[j ^ 1] * t.s[j];
     } else {
-        const bool second = l >= L / 2;
+        // the partners as they were read (half the exchange), with their own weights
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const R o = __shfl_xor(x[j], L / 2);
-            const double2 t = cs[(8 * l + j) % (D / 2)];
-            y[j] = x[j] * (R)t.x + (second ? o : -o) * (R)t.y;
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t o = across<L>(raw[j]);
+            R a = (R)lo_f32(o), b = (R)hi_f32(o);
+            if (w.on) {
+                a *= inv * w.other[2 * j];
+                b *= inv * w.other[2 * j + 1];
+            }
+            y[2 * j] = x[2 * j] * t.c[2 * j] + a * t.s[2 * j];
+            y[2 * j + 1] = x[2 * j + 1] * t.c[2 * j + 1] + b * t.s[2 * j + 1];
         }
     }
 }
@@ -133,15 +192,18 @@ template <int D> __device__ inline uint32_t get_v(const uint8_t* part, int k, in
            (uint32_t)*reinterpret_cast<const uint16_t*>(v + Part<D>::v_at(k, 8 * l + 4)) << 16;
 }
 
+// A workgroup takes TPW tokens.  Rows of queries (and of keys that stay bf16) go through its lane groups four at a time, then those that
+// end in the cache, keys and values of a token side by side.
 template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
 {
-    constexpr int L = D / 8, ROWS = 256 / L, P = D / 2;
+    constexpr int L = D / 8, ROWS = 256 / L, P = D / 2, U = 4;
     __shared__ double2 cs[TPW][P];
     const int t0 = blockIdx.x * TPW;
     const int T = a.cache ? min(a.T, a.head->rows) : a.T;
     if (t0 >= T) return;
     const int count = min(TPW, T - t0);
     const bool rotate = a.inv_freq != nullptr;
+    const int l = threadIdx.x % L, group = threadIdx.x / L;
     if (rotate) {
         for (int k = threadIdx.x; k < count * P; k += 256) {
             double s, c;
@@ -150,44 +212,62 @@ template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(He
         }
         __syncthreads();
     }
-    const int l = threadIdx.x % L;
-    const int nq = a.q ? a.n_heads : 0, nk = a.k ? a.n_kv : 0, nv = a.v ? a.n_kv : 0;
-    const int per = nq + nk + nv;
+
+    auto dense = [&](const uint16_t* in, int64_t in_stride, uint16_t* out, int64_t out_stride, const uint16_t* weight, int heads) {
+        Weights<float> w;
+        load_weights<D>(w, weight);
+        for (int tt = 0; tt < count; ++tt) {
+            const size_t t = t0 + tt;
+            const bool kept = !a.slot || a.slot[t] >= 0;
+            Turn<D, float> turn;
+            if (rotate) load_turn<D>(turn, cs[tt], a.pairs);
+            const uint16_t* from = in + t * in_stride + 8 * l;
+            uint16_t* to = out + t * out_stride + 8 * l;
+            for (int h0 = group; h0 < heads; h0 += U * ROWS) {
+                u32x4 raw[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (h0 + u * ROWS < heads) raw[u] = load16(from + (size_t)(h0 + u * ROWS) * D);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (h0 + u * ROWS >= heads) continue;
+                    float y[8];
+                    norm_rotate<D, float>(raw[u], w, a.eps, turn, rotate, a.pairs, y);
+                    u32x4 o;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = kept ? pack_bf16(y[2 * j], y[2 * j + 1]) : 0u;
+                    *reinterpret_cast<u32x4*>(to + (size_t)(h0 + u * ROWS) * D) = o;
+                }
+            }
+        }
+    };
+    if (a.q) dense(a.q, a.q_stride, a.q_out, a.q_out_stride, a.q_norm, a.n_heads);
+    if (!a.cache) {
+        if (a.k) dense(a.k, a.k_stride, a.k_out, a.k_out_stride, a.k_norm, a.n_kv);
+        return;
+    }
+
+    Weights<double> w;
+    load_weights<D>(w, a.k_norm);
     bool odd = false;
-    for (int r = threadIdx.x / L; r < count * per; r += ROWS) {
+    const int per = 2 * a.n_kv;
+    for (int r = group; r < count * per; r += ROWS) {
         const int tt = r / per, h = r - tt * per;
         const size_t t = t0 + tt;
-        if (h < nq) {
-            const bool kept = !a.slot || a.slot[t] >= 0;
-            float y[8];
-            norm_rotate<D, float>(load16(a.q + t * a.q_stride + (size_t)h * D + 8 * l), a.q_norm, a.eps, cs[tt], rotate, a.pairs, y);
-            u32x4 o;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = kept ? pack_bf16(y[2 * j], y[2 * j + 1]) : 0u;
-            *reinterpret_cast<u32x4*>(a.q_out + t * a.q_out_stride + (size_t)h * D + 8 * l) = o;
-            continue;
-        }
-        const bool is_k = h < nq + nk;
-        const int hk = is_k ? h - nq : h - nq - nk;
-        if (is_k && !a.cache) {
-            float y[8];
-            norm_rotate<D, float>(load16(a.k + t * a.k_stride + (size_t)hk * D + 8 * l), a.k_norm, a.eps, cs[tt], rotate, a.pairs, y);
-            u32x4 o;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = pack_bf16(y[2 * j], y[2 * j + 1]);
-            *reinterpret_cast<u32x4*>(a.k_out + t * a.k_out_stride + (size_t)hk * D + 8 * l) = o;
-            continue;
-        }
-        // into the cache (all lanes of a row agree on what follows)
-        const int slot = a.slot[t];
+        const bool is_k = h < a.n_kv;
+        const int hk = is_k ? h : h - a.n_kv;
+        const int slot = a.slot[t];                    // (all lanes of a row agree on what follows)
+        if (slot < 0) continue;
         float v[8];
+        const u32x4 raw = load16((is_k ? a.k + t * a.k_stride : a.v + t * a.v_stride) + (size_t)hk * D + 8 * l);
         if (is_k) {
+            Turn<D, double> turn;
             double y[8];
-            norm_rotate<D, double>(load16(a.k + t * a.k_stride + (size_t)hk * D + 8 * l), a.k_norm, a.eps, cs[tt], rotate, a.pairs, y);
+            if (rotate) load_turn<D>(turn, cs[tt], a.pairs);
+            norm_rotate<D, double>(raw, w, a.eps, turn, rotate, a.pairs, y);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = (float)y[j];
         } else {
-            const u32x4 raw = load16(a.v + t * a.v_stride + (size_t)hk * D + 8 * l);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v[2 * j] = lo_f32(raw[j]);
@@ -195,10 +275,7 @@ template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(He
             }
         }
         int exponent;
-        bool bad = false;
-        const uint32_t codes = to_codes(v, exponent, bad);
-        if (slot < 0) continue;
-        odd |= bad;
+        const uint32_t codes = to_codes(v, exponent, odd);
         uint8_t* part = a.cache + ((size_t)(slot / kBlock) * a.n_kv + hk) * Part<D>::kBytes;
         const int k = slot % kBlock;
         if (is_k) *reinterpret_cast<uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l) = codes;

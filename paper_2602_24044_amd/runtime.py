@@ -320,39 +320,57 @@ class ModelSession:
 
 
 # ---- key/value cache in four bits ----
-def _stream_of(stream: Optional[torch.cuda.Stream]) -> int:
-    return (stream or torch.cuda.current_stream()).cuda_stream
+class _On:
+    """The device as the current one, for as long as it is not already."""
+    __slots__ = ("other",)
+
+    def __init__(self, device: torch.device):
+        self.other = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *e):
+        if self.other is not None:
+            self.other.__exit__(*e)
 
 
-def _rows(t: torch.Tensor, width: int, rows: int, device, what: str) -> int:
+def _stream_of(stream: Optional[torch.cuda.Stream], device: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def _rows(t: torch.Tensor, rows: int, width: int, device, what: str) -> int:
     """Stride in elements between the rows of a bf16 operand [rows, width] whose rows are contiguous; raises ValueError."""
-    if t.dtype != torch.bfloat16 or t.device != device or t.dim() != 2 or t.shape != (rows, width):
+    if t.dtype is not torch.bfloat16 or t.device != device or t.shape != (rows, width):
         raise ValueError(f"{what}: bf16 [{rows}, {width}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.stride(1) != 1 or (rows > 1 and t.stride(0) < width):
+    stride, one = t.stride()
+    if one != 1 or (rows > 1 and stride < width):
         raise ValueError(f"{what}: the values of a row must lie next to each other, and rows must not overlap")
-    return t.stride(0) if rows > 1 else width
+    return stride if rows > 1 else width
 
 
-def _ints(t: torch.Tensor, n: Optional[int], device, what: str) -> torch.Tensor:
-    if t.dtype != torch.int32 or t.device != device or t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
-        raise ValueError(f"{what}: contiguous int32 [{'n' if n is None else n}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t
+def _ints(t: torch.Tensor, n: int, device, what: str) -> int:
+    """Address of a contiguous int32 operand [n] (0 if it is empty); raises ValueError."""
+    if t.dtype is not torch.int32 or t.device != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous int32 [{n}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _heads(dim: int, device, inv_freq, q_norm, k_norm, eps: float, pairing: int) -> B.lora_heads:
-    h = B.lora_heads()
-    if inv_freq is not None:
-        if inv_freq.dtype != torch.float32 or inv_freq.device != device or inv_freq.shape != (dim // 2,) or not inv_freq.is_contiguous():
-            raise ValueError(f"inv_freq: contiguous float32 [{dim // 2}] on {device} expected")
-        h.d_inv_freq = inv_freq.data_ptr()
-    for w, name in ((q_norm, "d_q_norm"), (k_norm, "d_k_norm")):
-        if w is not None:
-            if w.dtype != torch.bfloat16 or w.device != device or w.shape != (dim,) or not w.is_contiguous():
-                raise ValueError(f"{name[2:]}: contiguous bfloat16 [{dim}] on {device} expected")
-            setattr(h, name, w.data_ptr())
-    h.eps = float(eps)
-    h.pairing = int(pairing)
-    return h
+def _weight(t: Optional[torch.Tensor], n: int, dtype, device, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.device != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {dtype} [{n}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _heads(dim: int, device, inv_freq, q_norm, k_norm, eps: float, pairing: int, q=(None, 0), k=(None, 0), v=(None, 0),
+           q_out=(None, 0), k_out=(None, 0)) -> B.lora_heads:
+    """Each of q .. k_out: (address, stride)."""
+    return B.lora_heads(q[0], k[0], v[0], q[1], k[1], v[1], q_out[0], k_out[0], q_out[1], k_out[1],
+                        _weight(q_norm, dim, torch.bfloat16, device, "q_norm"), _weight(k_norm, dim, torch.bfloat16, device, "k_norm"),
+                        eps, _weight(inv_freq, dim // 2, torch.float32, device, "inv_freq"), pairing)
 
 
 def rotary_inv_freq(head_dim: int, base: float, device) -> torch.Tensor:
@@ -367,38 +385,52 @@ def head_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], n_hea
                      pairing: int = B.LORA_ROTATE_HALVES, q_out: Optional[torch.Tensor] = None,
                      k_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Norm and rotation of q [T, n_heads * dim] and k [T, n_kv_heads * dim] (lora_head_norm_rotate); returns the outputs."""
-    some = q if q is not None else k
-    if some is None or some.dim() != 2:
-        raise ValueError("q or k: bf16 [T, heads * dim] expected")
-    T, device = some.shape[0], some.device
-    dim = some.shape[1] // max(n_heads if q is not None else n_kv_heads, 1)
-    h = _heads(dim, device, inv_freq, q_norm, k_norm, eps, pairing)
-    with torch.cuda.device(device):
+    some, heads = (q, n_heads) if q is not None else (k, n_kv_heads)
+    if some is None or some.dim() != 2 or heads < 1 or not some.is_cuda:
+        raise ValueError("q or k: bf16 [T, heads * dim] on a GPU expected")
+    T, device, dim = some.shape[0], some.device, some.shape[1] // heads
+    with _On(device):
+        at = {"q": (None, 0), "k": (None, 0), "q_out": (None, 0), "k_out": (None, 0)}
         if q is not None:
             q_out = torch.empty((T, n_heads * dim), dtype=torch.bfloat16, device=device) if q_out is None else q_out
-            h.d_q, h.q_stride = q.data_ptr(), _rows(q, n_heads * dim, T, device, "q")
-            h.d_q_out, h.q_out_stride = q_out.data_ptr(), _rows(q_out, n_heads * dim, T, device, "q_out")
+            at["q"] = q.data_ptr(), _rows(q, T, n_heads * dim, device, "q")
+            at["q_out"] = q_out.data_ptr(), _rows(q_out, T, n_heads * dim, device, "q_out")
         if k is not None:
             k_out = torch.empty((T, n_kv_heads * dim), dtype=torch.bfloat16, device=device) if k_out is None else k_out
-            h.d_k, h.k_stride = k.data_ptr(), _rows(k, n_kv_heads * dim, T, device, "k")
-            h.d_k_out, h.k_out_stride = k_out.data_ptr(), _rows(k_out, n_kv_heads * dim, T, device, "k_out")
+            at["k"] = k.data_ptr(), _rows(k, T, n_kv_heads * dim, device, "k")
+            at["k_out"] = k_out.data_ptr(), _rows(k_out, T, n_kv_heads * dim, device, "k_out")
+        h = _heads(dim, device, inv_freq, q_norm, k_norm, eps, pairing, **at)
         if T:
-            d_pos = 0 if position is None else _ints(position, T, device, "position").data_ptr()
-            B.lora_head_norm_rotate(T, n_heads, n_kv_heads, dim, d_pos, h, _stream_of(stream))
+            d_pos = 0 if position is None else _ints(position, T, device, "position")
+            B.lora_head_norm_rotate(T, n_heads, n_kv_heads, dim, d_pos, h, _stream_of(stream, device))
     return q_out, k_out
 
 
 class KvStep:
-    """The step of the latest KvCache.extend: its arrays as tensors on the cache's memory."""
+    """The step of a KvCache.extend: its arrays as tensors on the cache's memory, good until the cache's next extend or release."""
 
-    def __init__(self, kv: "KvCache", raw: B.lora_kv_step):
-        self.raw = raw
-        self.n, self.T = int(raw.n), int(raw.T)
-        self.start = kv._view(raw.start, self.n + 1)
-        self.position = kv._view(raw.position, self.T)
-        self.slot = kv._view(raw.slot, self.T)
-        self.table = kv._view(raw.table, kv.max_seqs * int(raw.row_blocks)).view(kv.max_seqs, int(raw.row_blocks))
-        self.held = kv._view(raw.held, kv.max_seqs)
+    def __init__(self, arrays: Dict[str, torch.Tensor], raw: B.lora_kv_step, n: int, T: int):
+        self._arrays, self.raw, self.n, self.T = arrays, raw, n, T
+
+    @property
+    def start(self) -> torch.Tensor:
+        return self._arrays["start"][:self.n + 1]
+
+    @property
+    def position(self) -> torch.Tensor:
+        return self._arrays["position"][:self.T]
+
+    @property
+    def slot(self) -> torch.Tensor:
+        return self._arrays["slot"][:self.T]
+
+    @property
+    def table(self) -> torch.Tensor:
+        return self._arrays["table"]
+
+    @property
+    def held(self) -> torch.Tensor:
+        return self._arrays["held"]
 
 
 class KvCache:
@@ -414,15 +446,17 @@ class KvCache:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
-        self.n_blocks, self.max_seqs = n_blocks, max_seqs
+        self.n_blocks, self.max_seqs, self.max_tokens = n_blocks, max_seqs, max_tokens
+        self.q_width, self.k_width = n_heads * head_dim, n_kv_heads * head_dim
         cfg = B.make_kv_config(n_layers, n_heads, n_kv_heads, head_dim, n_blocks, max_seqs, max_seq_tokens, max_tokens)
         self.nbytes = B.lora_kv_slab_bytes(cfg)
-        with torch.cuda.device(self.device):
+        with _On(self.device):
             if self.nbytes:
                 self.slab = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
                 cfg.slab, cfg.slab_bytes = self.slab.data_ptr(), self.nbytes
             self.kv = B.lora_kv_create(cfg)       # says what is wrong with a shape that has no slab
         self.step: Optional[KvStep] = None
+        self._arrays: Dict[str, torch.Tensor] = {}
 
     def _view(self, ptr: int, n: int) -> torch.Tensor:
         off = int(ptr) - self.slab.data_ptr()
@@ -437,20 +471,24 @@ class KvCache:
     def extend(self, seq: torch.Tensor, length: torch.Tensor, new: torch.Tensor, T: int, max_new: Optional[int] = None,
                stream: Optional[torch.cuda.Stream] = None) -> KvStep:
         """Blocks and places for the next `new[i]` tokens of the sequences in rows `seq[i]`, which have `length[i]` tokens."""
-        n = int(seq.shape[0])
-        ptr = [_ints(t, n, self.device, what).data_ptr() if n else 0 for t, what in ((seq, "seq"), (length, "length"), (new, "new"))]
-        with torch.cuda.device(self.device):
-            raw = B.lora_kv_extend(self.kv, n, *ptr, T, T if max_new is None else max_new, _stream_of(stream))
-        self.step = KvStep(self, raw)
+        n = len(seq)
+        d_seq, d_len, d_new = (_ints(t, n, self.device, what) for t, what in ((seq, "seq"), (length, "length"), (new, "new")))
+        with _On(self.device):
+            raw = B.lora_kv_extend(self.kv, n, d_seq, d_len, d_new, T, T if max_new is None else max_new, _stream_of(stream, self.device))
+        if not self._arrays:                      # (the same memory for every step)
+            self._arrays = {"start": self._view(raw.start, self.max_seqs + 1), "position": self._view(raw.position, self.max_tokens),
+                            "slot": self._view(raw.slot, self.max_tokens), "held": self._view(raw.held, self.max_seqs),
+                            "table": self._view(raw.table, self.max_seqs * raw.row_blocks).view(self.max_seqs, raw.row_blocks)}
+        self.step = KvStep(self._arrays, raw, n, T)
         return self.step
 
     def release(self, seq: torch.Tensor, keep: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
         """Gives back the blocks of the rows `seq` behind their first `keep[i]` tokens (none are kept without `keep`)."""
-        n = int(seq.shape[0])
-        d_seq = _ints(seq, n, self.device, "seq").data_ptr() if n else 0
-        d_keep = _ints(keep, n, self.device, "keep").data_ptr() if n and keep is not None else 0
-        with torch.cuda.device(self.device):
-            B.lora_kv_release(self.kv, n, d_seq, d_keep, _stream_of(stream))
+        n = len(seq)
+        d_seq = _ints(seq, n, self.device, "seq")
+        d_keep = 0 if keep is None else _ints(keep, n, self.device, "keep")
+        with _On(self.device):
+            B.lora_kv_release(self.kv, n, d_seq, d_keep, _stream_of(stream, self.device))
         self.step = None
 
     def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -458,44 +496,43 @@ class KvCache:
               k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, pairing: int = B.LORA_ROTATE_HALVES,
               out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
         """The step's keys (normed, rotated) and values into the layer's cache; returns the normed and rotated queries."""
-        step = self._current_step()
-        h = _heads(self.head_dim, self.device, inv_freq, q_norm, k_norm, eps, pairing)
-        wq, wk = self.n_heads * self.head_dim, self.n_kv_heads * self.head_dim
-        with torch.cuda.device(self.device):
-            h.d_k, h.k_stride = k.data_ptr(), _rows(k, wk, step.T, self.device, "k")
-            h.d_v, h.v_stride = v.data_ptr(), _rows(v, wk, step.T, self.device, "v")
+        step, dev = self._current_step(), self.device
+        T = step.T
+        with _On(dev):
+            at = {"k": (k.data_ptr(), _rows(k, T, self.k_width, dev, "k")), "v": (v.data_ptr(), _rows(v, T, self.k_width, dev, "v"))}
             if q is not None:
-                out = torch.empty((step.T, wq), dtype=torch.bfloat16, device=self.device) if out is None else out
-                h.d_q, h.q_stride = q.data_ptr(), _rows(q, wq, step.T, self.device, "q")
-                h.d_q_out, h.q_out_stride = out.data_ptr(), _rows(out, wq, step.T, self.device, "out")
-            B.lora_kv_store(self.kv, layer, step.raw, h, _stream_of(stream))
+                out = torch.empty((T, self.q_width), dtype=torch.bfloat16, device=dev) if out is None else out
+                at["q"] = q.data_ptr(), _rows(q, T, self.q_width, dev, "q")
+                at["q_out"] = out.data_ptr(), _rows(out, T, self.q_width, dev, "out")
+            h = _heads(self.head_dim, dev, inv_freq, q_norm, k_norm, eps, pairing, **at)
+            B.lora_kv_store(self.kv, layer, step.raw, h, _stream_of(stream, self.device))
         return out
 
     def attend(self, layer: int, q: torch.Tensor, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Attention of the step's tokens over the layer's cache; scale: 1 / sqrt(head_dim) unless given."""
-        step = self._current_step()
-        w = self.n_heads * self.head_dim
-        with torch.cuda.device(self.device):
-            out = torch.empty((step.T, w), dtype=torch.bfloat16, device=self.device) if out is None else out
+        step, dev = self._current_step(), self.device
+        T, w = step.T, self.q_width
+        with _On(dev):
+            out = torch.empty((T, w), dtype=torch.bfloat16, device=dev) if out is None else out
             B.lora_kv_attend(self.kv, layer, step.raw, self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(),
-                             _rows(q, w, step.T, self.device, "q"), _rows(out, w, step.T, self.device, "out"), _stream_of(stream))
+                             _rows(q, T, w, dev, "q"), _rows(out, T, w, dev, "out"), _stream_of(stream, self.device))
         return out
 
     def read(self, layer: int, seq: torch.Tensor, position: torch.Tensor, stream: Optional[torch.cuda.Stream] = None):
         """Keys and values of the tokens (seq[i], position[i]) as the bf16 values that their codes stand for."""
-        n = int(seq.shape[0])
-        with torch.cuda.device(self.device):
-            k, v = (torch.empty((n, self.n_kv_heads * self.head_dim), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        n, dev = len(seq), self.device
+        with _On(dev):
+            k, v = (torch.empty((n, self.k_width), dtype=torch.bfloat16, device=dev) for _ in range(2))
             if n:
-                B.lora_kv_read(self.kv, layer, n, _ints(seq, n, self.device, "seq").data_ptr(),
-                               _ints(position, n, self.device, "position").data_ptr(), k.data_ptr(), v.data_ptr(), _stream_of(stream))
+                B.lora_kv_read(self.kv, layer, n, _ints(seq, n, dev, "seq"), _ints(position, n, dev, "position"), k.data_ptr(), v.data_ptr(),
+                               _stream_of(stream, self.device))
         return k, v
 
     def poll(self, stream: Optional[torch.cuda.Stream] = None):
         """(status, flag word) since the last poll."""
-        with torch.cuda.device(self.device):
-            return B.lora_kv_poll_flags(self.kv, _stream_of(stream))
+        with _On(self.device):
+            return B.lora_kv_poll_flags(self.kv, _stream_of(stream, self.device))
 
     def close(self):
         if self.kv:
