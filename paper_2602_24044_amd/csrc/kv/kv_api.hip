@@ -266,6 +266,7 @@ lora_status lora_kv_extend(lora_kv* k, int32_t n, const int32_t* d_seq, const in
     a.max_new = std::min(max_new, T);
     a.n_kv = k->cfg.n_kv_heads;
     a.group = k->cfg.n_heads / k->cfg.n_kv_heads;
+    a.whole = 0;
     if (KV_HIP_FAIL(launch_plan(a, s))) return LORA_ERR_HIP;
     k->step_n = n;
     k->step_T = T;

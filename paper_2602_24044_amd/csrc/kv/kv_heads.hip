@@ -79,6 +79,18 @@ template <int L> __device__ inline double row_sum(double v)
     return v;
 }
 
+__device__ inline float reciprocal_root(float x) { return __builtin_amdgcn_rsqf(x); }
+// The unit's estimate has some 23 bits or more: two Newton steps, y += y (1 - x y^2) / 2.  (Zero and infinity keep what the estimate says.)
+__device__ inline double reciprocal_root(double x)
+{
+    double y = __builtin_amdgcn_rsq(x);
+    if (y < 1e300 && y > 0.0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) y = __builtin_fma(0.5 * y, __builtin_fma(-x * y, y, 1.0), y);
+    }
+    return y;
+}
+
 // What a lane needs for every row of a token: cos and sin of its pairs, and with a norm the weights of its values and of those of the lane that
 // has their partners.  R = float (queries, and keys that stay bf16) or double (keys on their way to four bits).
 template <int D, typename R> struct Turn {
@@ -130,9 +142,7 @@ __device__ inline void norm_rotate(const u32x4 raw, const Weights<R>& w, float e
         R sum = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
-        const R mean = row_sum<L>(sum) / (R)D + (R)eps;
-        if constexpr (sizeof(R) == 8) inv = 1.0 / __builtin_sqrt(mean);
-        else inv = 1.0f / __builtin_sqrtf(mean);
+        inv = reciprocal_root(row_sum<L>(sum) * (R)(1.0 / D) + (R)eps);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] *= inv * w.own[j];
     }
@@ -194,12 +204,12 @@ template <int D> __device__ inline uint32_t get_v(const uint8_t* part, int k, in
 
 // A workgroup takes TPW tokens.  Rows of queries (and of keys that stay bf16) go through its lane groups four at a time, then those that
 // end in the cache, keys and values of a token side by side.
-template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
+template <int D, int TPW, bool CACHE> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
 {
     constexpr int L = D / 8, ROWS = 256 / L, P = D / 2, U = 4;
     __shared__ double2 cs[TPW][P];
     const int t0 = blockIdx.x * TPW;
-    const int T = a.cache ? min(a.T, a.head->rows) : a.T;
+    const int T = CACHE ? min(a.T, a.head->rows) : a.T;
     if (t0 >= T) return;
     const int count = min(TPW, T - t0);
     const bool rotate = a.inv_freq != nullptr;
@@ -218,7 +228,7 @@ template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(He
         load_weights<D>(w, weight);
         for (int tt = 0; tt < count; ++tt) {
             const size_t t = t0 + tt;
-            const bool kept = !a.slot || a.slot[t] >= 0;
+            const bool kept = !CACHE || a.slot[t] >= 0;
             Turn<D, float> turn;
             if (rotate) load_turn<D>(turn, cs[tt], a.pairs);
             const uint16_t* from = in + t * in_stride + 8 * l;
@@ -242,7 +252,7 @@ template <int D, int TPW> __global__ __launch_bounds__(256) void heads_kernel(He
         }
     };
     if (a.q) dense(a.q, a.q_stride, a.q_out, a.q_out_stride, a.q_norm, a.n_heads);
-    if (!a.cache) {
+    if constexpr (!CACHE) {
         if (a.k) dense(a.k, a.k_stride, a.k_out, a.k_out_stride, a.k_norm, a.n_kv);
         return;
     }
@@ -317,8 +327,14 @@ template <int D> __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 template <int D> hipError_t heads(const HeadsArgs& a, hipStream_t stream)
 {
     // a token of its own per workgroup while that fills no more than the chip; then four, whose angles keep all threads busy
-    if (a.T <= 1024) heads_kernel<D, 1><<<a.T, 256, 0, stream>>>(a);
-    else heads_kernel<D, 4><<<(a.T + 3) / 4, 256, 0, stream>>>(a);
+    const int wgs = a.T <= 1024 ? a.T : (a.T + 3) / 4;
+    if (a.cache) {
+        if (a.T <= 1024) heads_kernel<D, 1, true><<<wgs, 256, 0, stream>>>(a);
+        else heads_kernel<D, 4, true><<<wgs, 256, 0, stream>>>(a);
+    } else {
+        if (a.T <= 1024) heads_kernel<D, 1, false><<<wgs, 256, 0, stream>>>(a);
+        else heads_kernel<D, 4, false><<<wgs, 256, 0, stream>>>(a);
+    }
     return hipGetLastError();
 }
 template <int D> hipError_t read(const ReadArgs& a, hipStream_t stream)

@@ -48,6 +48,50 @@ __device__ inline void scan(int (&v)[N], int (&total)[N], int (*sums)[N])
     }
 }
 
+// What the plan has decided, written out.  Position and slot of row j of a request; entry k of its list of pieces.
+__device__ inline void write_row(const Tables& t, const Request& q, const int32_t* row, int j)
+{
+    int position = -1, slot = -1;
+    if (q.held >= 0) {
+        position = q.len + j;
+        const int b = position / kBlock;
+        slot = (b < q.held ? row[b] : t.fresh[q.fresh + b - q.held]) * kBlock + position % kBlock;
+    }
+    t.position[q.first + j] = position;
+    t.slot[q.first + j] = slot;
+}
+__device__ inline void write_entry(const Tables& t, const Request& q, const int32_t* row, int group, int k)
+{
+    const int cols = q.many ? kManyCols : kFewCols;
+    Entry e = {};
+    e.first = q.first;
+    e.rows = q.rows;
+    e.len = q.len;
+    e.row = q.held >= 0 ? q.row : 0;
+    e.tile = q.tiles - 1 - k / q.splits;               // the last tiles see the most keys: they come first
+    e.block = (k % q.splits) * q.chunk;
+    // the last token of the tile sees this many blocks
+    const int last = min(q.rows - 1, ((e.tile + 1) * cols - 1) / group);
+    const int seen = q.held >= 0 ? (q.len + last) / kBlock + 1 : 0;
+    e.blocks = max(0, min(q.chunk, seen - e.block));
+    e.part = q.splits > 1 ? q.part + k : -1;
+#pragma unroll
+    for (int j = 0; j < kEntryIds; ++j) {
+        const int b = e.block + j;
+        if (j < e.blocks) e.id[j] = b < q.held ? row[b] : t.fresh[q.fresh + b - q.held];
+    }
+    (q.many ? t.many : t.few)[q.entry + k] = e;
+}
+__device__ inline int merge_columns(const Request& q) { return q.splits < kMergeMany ? kMergeCols : 1; }
+__device__ inline void write_merge(const Tables& t, const Request& q, int k)
+{
+    const int together = merge_columns(q), place = q.tiles - 1 - k * together / (q.many ? kManyCols : kFewCols);
+    t.merge[q.merge + k] = Merge{q.first, q.rows, k * together, together, q.part + place * q.splits, q.splits, q.many, 0};
+}
+__device__ inline int32_t* table_row(const Tables& t, const Request& q) { return t.table + (size_t)(q.held >= 0 ? q.row : 0) * t.row_blocks; }
+
+// A step of up to kPlanThreads requests with a few tokens each is written out by the same workgroup, a thread per request and then per entry.
+constexpr int kSmallNew = 4;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
 {
     __shared__ int claim[kMaxSeqs];
@@ -190,7 +234,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
             v[1] = q.many ? pieces : 0;
             v[2] = q.splits > 1 ? v[0] : 0;
             v[3] = q.splits > 1 ? v[1] : 0;
-            const int together = q.splits < kMergeMany ? kMergeCols : 1;
+            const int together = merge_columns(q);
             v[4] = q.splits > 1 ? (q.rows * a.group + together - 1) / together : 0;
         }
         scan<5>(v, total, sums);
@@ -214,59 +258,55 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a)
         t.head->n_merge = at[4];
     }
     if (flags) atomicOr(&t.head->flags, flags);
+    if (!a.whole) return;
+
+    // (claim[] becomes the requests' first entries, in both lists together)
+    __syncthreads();
+    Request q = {};
+    if (tid < n) {
+        q = t.request[tid];
+        int32_t* row = table_row(t, q);
+        for (int j = 0; j < q.rows; ++j) write_row(t, q, row, j);
+        if (q.splits > 1)
+            for (int k = 0; k * merge_columns(q) < q.rows * a.group; ++k) write_merge(t, q, k);
+    }
+    int v[1] = {tid < n ? q.tiles * q.splits : 0}, total[1];
+    scan<1>(v, total, reinterpret_cast<int(*)[1]>(sums));
+    claim[tid] = v[0];
+    __syncthreads();
+    for (int e = tid; e < total[0]; e += kPlanThreads) {
+        int i = 0;                                     // the last request that begins at or before e
+#pragma unroll
+        for (int d = kPlanThreads / 2; d; d >>= 1)
+            if (i + d < n && claim[i + d] <= e) i += d;
+        const Request r = t.request[i];
+        write_entry(t, r, table_row(t, r), a.group, e - claim[i]);
+    }
+    __syncthreads();                                   // the table has been read: the blocks that the step takes
+    if (tid < n && q.held >= 0 && q.want > q.held) {
+        int32_t* row = table_row(t, q);
+        for (int b = q.held; b < q.want; ++b) row[b] = t.fresh[q.fresh + b - q.held];
+        t.held[q.row] = q.want;
+    }
 }
 
-// What plan_kernel has decided, written out: a workgroup per request and kFillRows of its token rows.
+// Longer steps: a workgroup per request and kFillRows of its token rows.
 constexpr int kFillRows = 1024;
 __global__ __launch_bounds__(256) void fill_kernel(PlanArgs a)
 {
     const Tables& t = a.t;
     const Request q = t.request[blockIdx.x];
-    int32_t* row = t.table + (size_t)(q.held >= 0 ? q.row : 0) * t.row_blocks;
+    int32_t* row = table_row(t, q);
     // (a refused request may have more rows than max_new, for which the grid was made)
-    for (int j = blockIdx.y * 256 + (int)threadIdx.x; j < q.rows; j += gridDim.y * 256) {
-        int position = -1, slot = -1;
-        if (q.held >= 0) {
-            position = q.len + j;
-            const int b = position / kBlock;
-            slot = (b < q.held ? row[b] : t.fresh[q.fresh + b - q.held]) * kBlock + position % kBlock;
-        }
-        t.position[q.first + j] = position;
-        t.slot[q.first + j] = slot;
-    }
+    for (int j = blockIdx.y * 256 + (int)threadIdx.x; j < q.rows; j += gridDim.y * 256) write_row(t, q, row, j);
     if (blockIdx.y) return;
     if (q.held >= 0) {
         for (int b = q.held + (int)threadIdx.x; b < q.want; b += 256) row[b] = t.fresh[q.fresh + b - q.held];
         if (threadIdx.x == 0) t.held[q.row] = q.want;
     }
-    // the last tiles see the most keys: they come first
-    const int cols = q.many ? kManyCols : kFewCols;
-    Entry* list = q.many ? t.many : t.few;
-    for (int k = threadIdx.x; k < q.tiles * q.splits; k += 256) {
-        Entry e = {};
-        e.first = q.first;
-        e.rows = q.rows;
-        e.len = q.len;
-        e.row = q.held >= 0 ? q.row : 0;
-        e.tile = q.tiles - 1 - k / q.splits;
-        e.block = (k % q.splits) * q.chunk;
-        // the last token of the tile sees this many blocks
-        const int last = min(q.rows - 1, ((e.tile + 1) * cols - 1) / a.group);
-        const int seen = q.held >= 0 ? (q.len + last) / kBlock + 1 : 0;
-        e.blocks = max(0, min(q.chunk, seen - e.block));
-        e.part = q.splits > 1 ? q.part + k : -1;
-        for (int j = 0; j < min(e.blocks, kEntryIds); ++j) {
-            const int b = e.block + j;
-            e.id[j] = b < q.held ? row[b] : t.fresh[q.fresh + b - q.held];
-        }
-        list[q.entry + k] = e;
-    }
-    const int together = q.splits < kMergeMany ? kMergeCols : 1;
+    for (int k = threadIdx.x; k < q.tiles * q.splits; k += 256) write_entry(t, q, row, a.group, k);
     if (q.splits > 1)
-        for (int k = threadIdx.x; k * together < q.rows * a.group; k += 256) {
-            const int place = q.tiles - 1 - k * together / cols;
-            t.merge[q.merge + k] = Merge{q.first, q.rows, k * together, together, q.part + place * q.splits, q.splits, q.many, 0};
-        }
+        for (int k = threadIdx.x; k * merge_columns(q) < q.rows * a.group; k += 256) write_merge(t, q, k);
 }
 
 __global__ __launch_bounds__(64) void release_kernel(Tables t, const int32_t* seq, const int32_t* keep)
@@ -294,8 +334,12 @@ __global__ __launch_bounds__(64) void release_kernel(Tables t, const int32_t* se
 
 hipError_t launch_plan(const PlanArgs& a, hipStream_t stream)
 {
-    plan_kernel<<<1, kPlanThreads, 0, stream>>>(a);
-    if (a.n > 0) {
+    // (T bounds what a refused request's rows cost one thread)
+    const bool whole = a.n <= kPlanThreads && a.T <= 4 * kPlanThreads && a.max_new <= kSmallNew;
+    PlanArgs b = a;
+    b.whole = whole;
+    plan_kernel<<<1, kPlanThreads, 0, stream>>>(b);
+    if (a.n > 0 && !whole) {
         const int chunks = std::max(1, (a.max_new + kFillRows - 1) / kFillRows);
         fill_kernel<<<dim3(a.n, chunks), 256, 0, stream>>>(a);
     }
