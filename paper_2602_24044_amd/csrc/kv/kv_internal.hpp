@@ -133,7 +133,7 @@ struct PlanArgs {
     const int32_t* add;
     int32_t n, T, max_new;
     int32_t n_kv, group;
-    int32_t whole;     // one workgroup does it all (launch_plan)
+    int32_t whole;     // the first launch writes everything out (launch_plan)
 };
 
 struct HeadsArgs {
