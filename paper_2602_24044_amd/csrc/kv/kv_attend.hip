@@ -3,17 +3,18 @@
 //   out[t, head] = sum_k p_k v_k,   p = softmax_k(scale q . k) over the keys at positions <= that of t
 //
 // in one pass over the keys: a running maximum m and sum l of the weights 2^(s - m), the accumulated values scaled down when m
-// grows.  Scores, weights' sums, m and the accumulated values are fp32; the weights are rounded to bf16 for the matrix units (2^-9 of
-// each, like the values' own rounding in a cache of 16 bits).
+// grows.  Scores, sums, m and the accumulated values are fp32; the weights are rounded to bf16 for the matrix units (2^-8 of each at
+// most, like the values' own rounding in a cache of 16 bits), and l is the sum of the rounded ones, so that equal values stay what they are.
 //
-// Two kernels share the work.  Of a request with few columns (one-token requests) a wave takes whole blocks and converts what it
-// needs itself: the cache's bytes bound it.  For long chunks four waves share the converted keys and values through LDS.
+// Two kernels share the work.  A tile of 16 columns is a wave's: requests with few queries, where the cache's bytes are the bound.
+// A tile of 128 columns is four waves', which share the converted values through LDS: chunks of prompts, where the matrix units and the
+// weights' exponentials are.
 //
 // A column is a query: (token j, head g of the key head's group), column j * group + g, so a group's heads share the keys that they
-// read.  S^T = K Q^T and O^T = V^T P^T on 16x16x32 MFMAs (32x32x16 in the second kernel): a lane's results belong to one column, the
-// accumulator of S^T (lane (c, quarter): keys 4 quarter + i of a 16-key tile) is the operand that the second product wants once its 32
-// keys are counted in that order, and the codes of four keys and eight dimensions that a lane loads with one instruction are
-// its own part of V^T, so neither the weights nor the values cross lanes or LDS.
+// read.  S^T = K Q^T on MFMAs that take the keys' four-bit codes and exponents as they are in the cache (16x16x128, 32x32x64), O^T = V^T
+// P^T on bf16 MFMAs (16x16x32, 32x32x16) with the values converted.  A lane's results belong to one column; the accumulator of S^T
+// (lane (column, quarter): keys 4 quarter + i of a 16-key tile) is the operand that the second product wants once its keys are counted in
+// that order, and the codes of four keys that a lane loads with one instruction are its own part of V^T, so the weights never cross lanes.
 #include "kv_device.hpp"
 
 #include <algorithm>

@@ -26,13 +26,21 @@ def f64(t):
     return t.detach().double().cpu().numpy()
 
 
-def attend_bound(out, size, top, n_keys, dim):
-    """How far an element of the attention's output may be from the float64 result.  Every weight is rounded to bf16 (HALF), and so is the
-    result; a score is a sum of dim products in fp32, off by (dim + 2) U32 top, and the weights are e^score, off by as much relative
-    to themselves, twice (in the sum and in its denominator); exp2 and the products around it: 4 U32 each way; sums over the keys in
-    fp32, with at most one rescaling per key: 2 n_keys U32, twice."""
-    wiggle = 2 * (dim + 2) * U32 * top + 8 * U32 + 4 * n_keys * U32
-    return (HALF + wiggle * (1 + HALF)) * size + HALF * np.abs(out) * (1 + HALF) + 1e-38
+def attend_bound(out, size, top, n_keys, dim, split):
+    """How far an element of the attention's output may be from the float64 result `out`; size: sum of the weights (which sum to 1)
+    times |values|; top: the largest sum |q k| of a score, scaled; split: the largest max|q| sum |k| of a score, scaled.
+
+    A score.  A query is taken as 2^n (a + b / 16) with a, b in e4m3 and 2^7 <= max|q| / 2^n < 2^8.  A bf16 value at or above 2^(n - 6) has its
+    last bit at or above 2^(n - 13), and what a leaves over is at most half a step of a, so b, whose smallest step is 2^-9 / 16 = 2^-13,
+    holds it exactly; a smaller value is off by half that step, 2^(n - 14) <= 2^-21 max|q|.  |a| + |b| / 16 <= (1 + 2 * 2^-4) |q|, so the 2 dim
+    products in fp32 sum to within 2 dim U32 1.125 top; the factor scale * log2(e), its product and the difference from
+    the running maximum are three roundings of at most 2 top: 6 U32 top.
+    A weight is e^score (exp2 and rescalings: 8 U32, and U32 per rescaling, of which there is at most one per key), relative to
+    itself, in the numerator and the denominator, and so is its rounding to bf16: with weights p (1 + d), |d| <= HALF,
+    sum p (1 + d) v / sum p (1 + d) - out = sum p d (v - out) / sum p (1 + d), at most HALF (size + |out|) / (1 - HALF).
+    Sums over the keys are fp32 (n_keys U32, twice), and the result is rounded once."""
+    wiggle = 2 * ((2 * dim * 1.125 + 6) * U32 * top + 2.0 ** -21 * split) + 16 * U32 + 4 * n_keys * U32
+    return (HALF / (1 - HALF) + wiggle * (1 + HALF)) * (size + np.abs(out)) + HALF * np.abs(out) * (1 + HALF) + 1e-38
 
 
 class Model:
@@ -84,6 +92,14 @@ class Model:
             self.put(layer, okv.four_bits(k64.astype(np.float32).astype(np.float64)), okv.four_bits(f64(v).reshape(self.T, self.kvh, self.dim)))
         return q
 
+    def release(self, seq, keep=None):
+        self.kv.release(i32(seq), None if keep is None else i32(keep))
+        self.tables.release(list(seq), keep)
+        assert np.array_equal(self.kv_table(), self.tables.table())
+
+    def kv_table(self):
+        return self.kv._arrays["table"].cpu().numpy()
+
     def fill(self, seq, length, layer=0, step=512):
         """Sequences of the given lengths, with random keys and values."""
         for r, n in zip(seq, length):
@@ -109,7 +125,9 @@ class Model:
             keys, values = (x[layer][r][:self.length[i] + b - a] for x in (self.keys, self.values))
             ref, size, top = okv.attend(f64(q[a:b]).reshape(b - a, h, d), keys, values, self.length[i], scale)
             assert np.array_equal(np.isnan(y), np.isnan(ref)), i
-            over = np.abs(y - ref) - attend_bound(ref, size, top, len(keys), d)
+            split = np.abs(scale) * np.abs(f64(q[a:b]).reshape(b - a, h, d)).max(axis=2, keepdims=True) * np.repeat(
+                np.abs(keys).sum(axis=2).max(axis=0), h // self.kvh)[None, :, None]
+            over = np.abs(y - ref) - attend_bound(ref, size, top, len(keys), d, split)
             assert not (over > 0).any(), (i, float(np.nanmax(over)), np.argwhere(over > 0)[:4].tolist())
         return got
 
