@@ -14,6 +14,9 @@ layer, a slot = one adapter's matrices of all layers) and computes the second:
   when it follows a load: after waiting for it, or enqueued straight behind it on another stream (the copies
   travel layer after layer and each layer's forward waits only for its own); each with the copy engine and
   with the copy kernel carrying the adapters (every adapter is one pinned buffer: one run per layer).
+* `cache_bytes` - bytes that the keys and values of a number of tokens take, in the cache of four bits (lora_kv_*) and in bf16,
+  and how many tokens fit into a slot's bytes: what the adapter region takes from.  Arithmetic on shapes only.
+* `measure_cache` - the decode step over all layers with attention over cached tokens.
 
 Weights and adapter values are random bits of the right shape, generated on the device / in pinned memory: only
 sizes and residency matter for these timings.
@@ -38,13 +41,72 @@ def slot_region_bytes(proj: Sequence[Tuple[int, int]], n_layers: int, ranks: Seq
             "per_rank_unit": int(per_rank)}
 
 
+def cache_bytes(n_layers: int, n_kv_heads: int, head_dim: int, n_tokens: int, slot_bytes: int = 0) -> Dict[str, int]:
+    """Bytes of the keys and values of `n_tokens` tokens of one sequence (whole blocks of 64), and tokens that `slot_bytes` hold."""
+    block = n_layers * n_kv_heads * 68 * head_dim
+    return {"four_bits": -(-n_tokens // 64) * block, "bf16": 4 * n_layers * n_kv_heads * head_dim * n_tokens,
+            "tokens_per_slot": slot_bytes // block * 64}
+
+
+def measure_cache(step, n_layers: int, n_tokens: int, context: int, reps: int) -> Dict[str, float]:
+    """step(cache): enqueues a decode step of `n_tokens` one-token requests with attention over `cache`, which holds `context`
+    tokens of each.  Times of the step and of attention's calls alone (ms), and the bytes of the cache."""
+    import torch
+
+    from .runtime import KvCache
+
+    dev = torch.device("cuda:0")
+    heads, kv, dim, chunk = 32, 8, 128, 8192
+    cache = KvCache(n_layers, heads, kv, dim, n_tokens * (context // 64 + 1), n_tokens, context + 64, chunk)
+    try:
+        k, v = (torch.empty((chunk, kv * dim), dtype=torch.bfloat16, device=dev).normal_() for _ in range(2))
+        rows = torch.arange(n_tokens, dtype=torch.int32, device=dev)
+        per = max(1, chunk // context)
+        assert context <= chunk
+        for r in range(0, n_tokens, per):
+            part = rows[r:r + per]
+            T = len(part) * context
+            cache.extend(part, torch.zeros_like(part), torch.full_like(part, context), T, context)
+            for l in range(n_layers):
+                cache.store(l, k[:T], v[:T])
+        length, new = torch.full_like(rows, context), torch.ones_like(rows)
+        q = torch.empty((n_tokens, heads * dim), dtype=torch.bfloat16, device=dev).normal_()
+        out = torch.empty_like(q)
+
+        def whole():
+            cache.extend(rows, length, new, n_tokens, 1)
+            step(cache)
+
+        def attention():
+            cache.extend(rows, length, new, n_tokens, 1)
+            for l in range(n_layers):
+                cache.store(l, k[:n_tokens], v[:n_tokens], q=q, out=out)
+                cache.attend(l, out, out=q)
+
+        res: Dict[str, float] = {"context": context, "cache_bytes": cache.nbytes}
+        for name, fn in (("step_ms", whole), ("attention_ms", attention)):
+            times = []
+            for _ in range(reps + 2):
+                torch.cuda.synchronize()
+                t0 = time.perf_counter()
+                fn()
+                torch.cuda.synchronize()
+                times.append((time.perf_counter() - t0) * 1e3)
+            res[name] = min(times)
+        if cache.poll()[1]:
+            raise RuntimeError("cache flags set during the measurement")
+        return res
+    finally:
+        cache.close()
+
+
 def measure(n_layers: int = 32, n_tokens: int = 256, n_slots: int = 32, n_swap: int = 8, reps: int = 3,
-            ranks: Sequence[int] = (8, 16, 32)) -> Dict[str, object]:
+            ranks: Sequence[int] = (8, 16, 32), context: int = 1024) -> Dict[str, object]:
     import torch
 
     from . import binding as B
     from . import workloads as wl
-    from .runtime import packed_groups
+    from .runtime import packed_groups, rotary_inv_freq
 
     dev = torch.device("cuda:0")
     torch.cuda.set_device(dev)
@@ -115,6 +177,25 @@ def measure(n_layers: int = 32, n_tokens: int = 256, n_slots: int = 32, n_swap: 
                 if l == 0 and after_layer0 is not None:
                     after_layer0.record(stream)
 
+        def step_with(cache):      # the same step with attention between q|k|v and o
+            q, k, v, o = (names.index(nm) for nm in ("q", "k", "v", "o"))
+            stream = torch.cuda.current_stream()
+            seg = B.lora_bucket(ctx, d_ids0.data_ptr(), n_tokens, wl.BUCKET_SORTED, stream.cuda_stream)
+            for l in range(n_layers):
+                def forward(g, inputs):
+                    B.lora_model_forward_group(ctx, l, g, inputs, [W[l][p].data_ptr() for p in g], seg,
+                                               [out[p].data_ptr() for p in g], stream.cuda_stream)
+                forward([q, k, v], [x[p].data_ptr() for p in (q, k, v)])
+                cache.store(l, out[k], out[v], q=out[q], inv_freq=freq, out=rotated)
+                cache.attend(l, rotated, out=mixed)
+                forward([o], [mixed.data_ptr()])
+                for g in groups:
+                    if not set(g) & {q, k, v, o}:
+                        forward(g, [x[p].data_ptr() for p in g])
+
+        freq = rotary_inv_freq(128, 500000.0, dev)
+        rotated, mixed = (torch.empty((n_tokens, 32 * 128), dtype=torch.bfloat16, device=dev) for _ in range(2))
+
         def ids_with(swap):      # the step's tokens once adapters 0 .. n_swap-1 have been replaced by `swap`
             ids = ids0.copy()
             for k, a in enumerate(swap):
@@ -184,6 +265,8 @@ def measure(n_layers: int = 32, n_tokens: int = 256, n_slots: int = 32, n_swap: 
                                 "load_then_step_ms": min(t_serial), "step_behind_load_ms": min(t_overlap),
                                 "first_layer_done_ms": min(t_first)}
         res["per_rank"] = per_rank
+        res["with_cache"] = measure_cache(step_with, n_layers, n_tokens, context, reps)
+        res["cache"] = cache_bytes(n_layers, 8, 128, context, 2 * n_layers * s_max * unit)
         a_maxes = [8, 32, 128, 384]
         mix = [int(v) for v in np.random.default_rng(0).choice(list(ranks), size=max(a_maxes))]
         res["slot_region"] = {str(a): slot_region_bytes(proj, n_layers, mix, s_max, a) for a in a_maxes}

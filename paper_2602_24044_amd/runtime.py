@@ -255,6 +255,7 @@ class ModelSession:
                     B.lora_set_bias(self.ctx, p, b.data_ptr(), layer=l)
         self.ids = torch.from_numpy(w.token_ids).to(self.device)
         self.groups = packed_groups(w)
+        self._heads: Optional[List[torch.Tensor]] = None      # rotated queries and attention's result, if there is a cache
         self.pinned: Dict[int, dict] = {}
         self.seg: Optional[B.lora_segments] = None
 
@@ -283,9 +284,12 @@ class ModelSession:
                                  self.w.mode, s)
         return self.seg
 
-    def forward_layer(self, l: int, stream: Optional[torch.cuda.Stream] = None) -> None:
+    def forward_layer(self, l: int, stream: Optional[torch.cuda.Stream] = None, without: Sequence[str] = ()) -> None:
+        """Layer l's projections, apart from those named in `without`."""
         s = (stream or torch.cuda.current_stream()).cuda_stream
         for g in self.groups:
+            if any(self.w.proj_names[p] in without for p in g):
+                continue
             B.lora_model_forward_group(self.ctx, l, g, [self.x[l][p].data_ptr() for p in g],
                                        [self.W[l][p].data_ptr() for p in g], self.seg,
                                        [self.out[l][p].data_ptr() for p in g], s)
@@ -301,11 +305,37 @@ class ModelSession:
                                  self.W[l][p_up].data_ptr(), self.seg, out.data_ptr(), s)
         return out
 
-    def step(self, stream: Optional[torch.cuda.Stream] = None) -> None:
-        """One step of the whole model: one segment map, then every layer's projections."""
+    def forward_attention(self, l: int, cache: "KvCache", scale: Optional[float] = None,
+                          stream: Optional[torch.cuda.Stream] = None, **rotation) -> torch.Tensor:
+        """Layer l from the inputs of q, k and v to its o projection: q|k|v, their heads normed and rotated and the keys and values stored
+        (`rotation`: inv_freq, q_norm, k_norm, eps, pairing of KvCache.store), attention over the cache, o on its result.
+        The step is the latest cache.extend's, of as many token rows as the session's."""
+        names = list(self.w.proj_names)
+        q, k, v, o = (names.index(nm) for nm in ("q", "k", "v", "o"))
+        if self.w.proj[q][1] != cache.q_width or self.w.proj[k][1] != cache.k_width or self.w.proj[v][1] != cache.k_width:
+            raise ValueError("the cache's heads are not those of the q, k and v projections")
+        if self._heads is None:
+            self._heads = [torch.empty((self.w.T, cache.q_width), dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+        rotated, mixed = self._heads
+        s = (stream or torch.cuda.current_stream()).cuda_stream
+        out = self.out[l]
+        B.lora_model_forward_group(self.ctx, l, [q, k, v], [self.x[l][p].data_ptr() for p in (q, k, v)],
+                                   [self.W[l][p].data_ptr() for p in (q, k, v)], self.seg,
+                                   [out[p].data_ptr() for p in (q, k, v)], s)
+        cache.store(l, out[k], out[v], q=out[q], out=rotated, stream=stream, **rotation)
+        cache.attend(l, rotated, scale, out=mixed, stream=stream)
+        B.lora_model_forward_group(self.ctx, l, [o], [mixed.data_ptr()], [self.W[l][o].data_ptr()], self.seg,
+                                   [out[o].data_ptr()], s)
+        return out[o]
+
+    def step(self, stream: Optional[torch.cuda.Stream] = None, cache: Optional["KvCache"] = None, **rotation) -> None:
+        """One step of the whole model: one segment map, then every layer's projections; with a cache, attention over it
+        between q|k|v and o (forward_attention)."""
         self.bucket(stream)
         for l in range(len(self.layers)):
-            self.forward_layer(l, stream)
+            if cache is not None:
+                self.forward_attention(l, cache, stream=stream, **rotation)
+            self.forward_layer(l, stream, without=() if cache is None else ("q", "k", "v", "o"))
 
     def close(self):
         if self.ctx:

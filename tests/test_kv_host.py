@@ -88,3 +88,12 @@ def test_status_strings():
     assert "refused" in B.lora_status_string(B.LORA_ERR_KV_REFUSED)
     assert "block" in B.lora_status_string(B.LORA_ERR_KV_EXHAUSTED)
     assert "finite" in B.lora_status_string(B.LORA_ERR_NOT_FINITE)
+
+
+def test_cache_bytes():
+    # two layers of three key heads of 64: a block of 64 tokens takes 2 * 3 * 64 * (64 + 4) bytes, 4.25 bits a value
+    from paper_2602_24044_amd.model_step import cache_bytes
+    r = cache_bytes(2, 3, 64, 65, slot_bytes=3 * 26112 - 1)
+    assert r["four_bits"] == 2 * 26112 and 26112 * 8 == 2 * 3 * 2 * 64 * 64 * 4.25
+    assert r["bf16"] == 65 * 2 * 3 * 2 * 64 * 2
+    assert r["tokens_per_slot"] == 128                   # whole blocks
