@@ -53,8 +53,12 @@ __device__ inline float max_quarters(float x)
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---- tiles of few columns ----
-// A wave takes a piece of a tile by itself, sixteen waves on a CU.  Its blocks are copied to LDS as they are, the next block's keys as
-// soon as this block's scores are there, its values at the end of the block: what is on its way hangs on no register.
+// A wave takes a piece of a tile by itself, eleven waves on a CU.  Its blocks are copied to LDS as they are, the next block's keys as
+// soon as this block's scores are there, its values at the end of the block: what is on its way hangs on no register (four waves that
+// share a tile's blocks and fetch them through registers: 91 us instead of 86 for 256 requests; one place for keys and sixteen waves a
+// CU: slower too).  The cache's bytes bound it: those 256 requests (378 MB) at 4.4 TB/s, one of 130000 tokens (141 MB) in 29 us, 4.8
+// TB/s.  The matrix units are busy for 16 % of that and the vector unit for 37 %; what is missing is that all pieces start at once and the
+// longest end alone.
 template <int D> struct Stage {
     static constexpr int kKeys = 2, kExpPlaces = 4;
     static constexpr int kHalf = kBlock * Part<D>::kRow, kExps = 2 * kBlock * Part<D>::kGroups;
@@ -409,6 +413,12 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 // Four waves of 32 columns each on 32x32 MFMAs.  A block's keys are copied to LDS as they are (four-bit operands); its values go through
 // registers, where each thread converts an eighth of 16 tokens to bf16 operands of V^T in LDS, once for all four waves.  Two stages: the next
 // block is made while this one is used.
+//
+// A prompt of 8192 tokens, 32 heads on 8 of 128 (550 GFLOP) takes 500 - 550 us: 1.0 - 1.1 PFLOP/s, where a large bf16 product reaches 1.25.
+// Matrix and vector units are busy for half of the time each and LDS for as much; leaving out any one of them (scores, exponentials,
+// conversion, products with the values) takes 5 - 17 % off, so it is the chain through all of them, twice on each SIMD, that counts.
+// Not kept: 64 columns a wave, alone on its SIMD (694 us: scores and sums change places between the two kinds of registers);
+// conversion and maximum between the products with the values (557); the conversion's lanes dealt out otherwise (570).
 //
 // Values, as the 256 threads load them: a chunk of four tokens, kE dimensions.  That is half of an operand of V^T for each of these: the
 // other half are the four tokens eight further.

@@ -4,12 +4,15 @@
 //   u = x / sqrt(mean(x^2) + eps) * w            (where there is a weight)
 //   y_p = u_p cos a - u_p' sin a,  y_p' = u_p' cos a + u_p sin a,   a = position * f_p,  p' = p + D/2 (or its neighbour)
 //
-// One read and one write of every head, so the copy rate bounds it.  D / 8 lanes share a head's row, 16 bytes each; the other half of
+// One read and one write of every head, so the copy rate bounds it: 4099 tokens of 32 + 8 heads of 128 with norm, 67 MB, in 17.8 us (3.8
+// TB/s), 8190 into the cache, 313 MB with the queries, in 74 (4.2 TB/s: the keys' double arithmetic and the codes keep the vector
+// unit busy for two thirds of it), out of it 16.5.  D / 8 lanes share a head's row, 16 bytes each; the other half of
 // a rotated pair sits D / 16 lanes away.  Angles are taken in 64 bits (a far position times a frequency has few bits left behind the
 // point in 32) once per token and pair, and shared by all heads through LDS.  Keys on the way to four bits are computed in 64 bits
 // throughout and rounded to 32 once: next to a border between two codes an error of 2^-24 would pick the wrong one now and then.
 #include "kv_device.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lora {
@@ -326,13 +329,15 @@ template <int D> __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 
 template <int D> hipError_t heads(const HeadsArgs& a, hipStream_t stream)
 {
-    // a token of its own per workgroup while that fills no more than the chip; then four, whose angles keep all threads busy
-    const int wgs = a.T <= 1024 ? a.T : (a.T + 3) / 4;
+    // A token of its own per workgroup, or four, whose angles keep all threads busy and whose norm weights are loaded once.  One / four,
+    // 32 + 8 heads of 128 out of HBM: rotation of 256 tokens 6.4 / 13.2 us, 2048 17.0 / 18.3, 4096 28.1 / 26.8; into the cache 2048
+    // tokens 21.7 / 23.8, 8192 76 / 71.
+    const int wgs = a.T <= 2048 ? a.T : (a.T + 3) / 4;
     if (a.cache) {
-        if (a.T <= 1024) heads_kernel<D, 1, true><<<wgs, 256, 0, stream>>>(a);
+        if (a.T <= 2048) heads_kernel<D, 1, true><<<wgs, 256, 0, stream>>>(a);
         else heads_kernel<D, 4, true><<<wgs, 256, 0, stream>>>(a);
     } else {
-        if (a.T <= 1024) heads_kernel<D, 1, false><<<wgs, 256, 0, stream>>>(a);
+        if (a.T <= 2048) heads_kernel<D, 1, false><<<wgs, 256, 0, stream>>>(a);
         else heads_kernel<D, 4, false><<<wgs, 256, 0, stream>>>(a);
     }
     return hipGetLastError();
@@ -340,8 +345,18 @@ template <int D> hipError_t heads(const HeadsArgs& a, hipStream_t stream)
 template <int D> hipError_t read(const ReadArgs& a, hipStream_t stream)
 {
     constexpr int rows = 256 / (D / 8);
-    const long n = (long)a.n * 2 * a.n_kv;
-    read_kernel<D><<<(unsigned)((n + rows - 1) / rows), 256, 0, stream>>>(a);
+    const int most = (1 << 26) / a.n_kv;               // tokens of a launch: its threads are counted in 32 bits
+    for (int at = 0; at < a.n; at += most) {
+        ReadArgs b = a;
+        const size_t skip = (size_t)at * a.n_kv * D;
+        b.n = std::min(most, a.n - at);
+        b.seq += at;
+        b.position += at;
+        b.k_out = a.k_out ? a.k_out + skip : nullptr;
+        b.v_out = a.v_out ? a.v_out + skip : nullptr;
+        const long n = (long)b.n * 2 * b.n_kv;
+        read_kernel<D><<<(unsigned)((n + rows - 1) / rows), 256, 0, stream>>>(b);
+    }
     return hipGetLastError();
 }
 

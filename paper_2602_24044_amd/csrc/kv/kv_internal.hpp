@@ -21,10 +21,14 @@ constexpr int kMaxTokens = 1 << 20;
 constexpr int kMaxHeads = 1024;
 constexpr int kPlanThreads = 1024;
 // Attention works on tiles of columns (token, query head of a key head).  Requests of up to kFewMost columns take tiles of
-// kFewCols, whose waves each convert the codes that they need; longer ones take tiles of kManyCols, whose waves share them.
+// kFewCols, whose waves each convert the codes that they need; longer ones take tiles of kManyCols, whose waves share them.  Where one
+// overtakes the other, with 32 query heads on 8 key heads of 128 (few / many columns, us): 40 columns, 256 requests with 200 cached
+// tokens 45 / 62, 64 with 1000 44 / 46, 4 with 1000 10 / 16; 64 columns, 64 with 1000 46 / 48; 128 columns 78 / 54.
 constexpr int kFewCols = 16, kManyCols = 128;
-constexpr int kFewMost = 32;
-// Pieces that the keys of the tiles are cut into, over all tiles and key heads; at most one more per tile (see plan_kernel).
+constexpr int kFewMost = 64;
+// Pieces that the keys of the tiles are cut into, over all tiles and key heads; at most one more per tile (piece_blocks).  Few columns:
+// eleven waves a CU find room, 256 requests of mixed lengths take 86 - 90 us with 2048 pieces and more with 1536 or 2816 - 6144.  Many
+// columns, 256 / 512 / 1024 pieces: 500 tokens behind 16000 178 / 160 / 172 us, 2000 tokens alone 60 / 60 / 70, and a merge of 7 / 9 / 12.
 constexpr int kFewItems = 2048, kManyItems = 512;
 constexpr int kFewChunk = 4, kManyChunk = 8;   // blocks of the smallest piece
 constexpr int kMinExp = -100, kMaxExp = 125;
@@ -90,7 +94,8 @@ struct Entry {
 };
 static_assert(sizeof(Entry) == 64, "one line");
 // Columns whose tile's range was split: the partial results are merged behind.  kMergeCols columns an entry, or one where there are at least
-// kMergeMany pieces (all lanes of a workgroup then work on it).
+// kMergeMany pieces (all lanes of a workgroup then work on it: 8 requests of 32 pieces 4.8 us, 7.9 with eight columns an entry; with four
+// pieces and more it is the same either way).
 constexpr int kMergeCols = 8, kMergeMany = 16;
 struct Merge {
     int32_t first, rows;   // as in Entry

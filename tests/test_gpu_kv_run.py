@@ -211,10 +211,11 @@ def test_steps_that_have_ended_are_refused():
         m.close()
 
 
-@pytest.mark.parametrize("heads,kv,past,new", [(8, 1, 300, 4), (8, 1, 300, 5), (1, 1, 500, 16), (1, 1, 500, 17), (1, 1, 500, 32), (1, 1, 500, 33),
-                                               (1, 1, 500, 128), (1, 1, 500, 129), (1024, 1, 200, 2), (100, 1, 0, 1)])
+@pytest.mark.parametrize("heads,kv,past,new", [(8, 1, 300, 4), (8, 1, 300, 5), (1, 1, 500, 16), (1, 1, 500, 17),
+                                               (1, 1, 500, 32), (1, 1, 500, 33), (8, 1, 300, 8), (8, 1, 300, 9), (1, 1, 500, 64),
+                                               (1, 1, 500, 65), (1, 1, 500, 128), (1, 1, 500, 129), (1024, 1, 200, 2), (100, 1, 0, 1)])
 def test_columns_on_both_sides_of_a_tile(heads, kv, past, new):
-    """Queries of a request that just fill tiles of 16, 32 and 128 columns, and one more; a thousand heads on one key head."""
+    """Queries of a request that just fill tiles of 16, 32, 64 and 128 columns, and one more; a thousand heads on one key head."""
     m = Model(heads, kv, 128, n_blocks=40, max_seqs=2, max_seq_tokens=1024, max_tokens=512, seed=new)
     try:
         m.fill([1], [past])
