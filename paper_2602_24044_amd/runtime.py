@@ -355,7 +355,7 @@ class _On:
     __slots__ = ("other",)
 
     def __init__(self, device: torch.device):
-        self.other = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        self.other = None if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
 
     def __enter__(self):
         if self.other is not None:
@@ -368,6 +368,13 @@ class _On:
 
 def _stream_of(stream: Optional[torch.cuda.Stream], device: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
+def _like(t: torch.Tensor, rows: int, width: int, device) -> torch.Tensor:
+    """An output [rows, width] beside the operand t.  (Shorter for the host where t itself is dense.)"""
+    if t.is_contiguous() and t.shape == (rows, width):
+        return torch.empty_like(t)
+    return torch.empty((rows, width), dtype=torch.bfloat16, device=device)
 
 
 def _rows(t: torch.Tensor, rows: int, width: int, device, what: str) -> int:
@@ -422,11 +429,11 @@ def head_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], n_hea
     with _On(device):
         at = {"q": (None, 0), "k": (None, 0), "q_out": (None, 0), "k_out": (None, 0)}
         if q is not None:
-            q_out = torch.empty((T, n_heads * dim), dtype=torch.bfloat16, device=device) if q_out is None else q_out
+            q_out = _like(q, T, n_heads * dim, device) if q_out is None else q_out
             at["q"] = q.data_ptr(), _rows(q, T, n_heads * dim, device, "q")
             at["q_out"] = q_out.data_ptr(), _rows(q_out, T, n_heads * dim, device, "q_out")
         if k is not None:
-            k_out = torch.empty((T, n_kv_heads * dim), dtype=torch.bfloat16, device=device) if k_out is None else k_out
+            k_out = _like(k, T, n_kv_heads * dim, device) if k_out is None else k_out
             at["k"] = k.data_ptr(), _rows(k, T, n_kv_heads * dim, device, "k")
             at["k_out"] = k_out.data_ptr(), _rows(k_out, T, n_kv_heads * dim, device, "k_out")
         h = _heads(dim, device, inv_freq, q_norm, k_norm, eps, pairing, **at)
@@ -531,7 +538,7 @@ class KvCache:
         with _On(dev):
             at = {"k": (k.data_ptr(), _rows(k, T, self.k_width, dev, "k")), "v": (v.data_ptr(), _rows(v, T, self.k_width, dev, "v"))}
             if q is not None:
-                out = torch.empty((T, self.q_width), dtype=torch.bfloat16, device=dev) if out is None else out
+                out = _like(q, T, self.q_width, dev) if out is None else out
                 at["q"] = q.data_ptr(), _rows(q, T, self.q_width, dev, "q")
                 at["q_out"] = out.data_ptr(), _rows(out, T, self.q_width, dev, "out")
             h = _heads(self.head_dim, dev, inv_freq, q_norm, k_norm, eps, pairing, **at)
@@ -544,7 +551,7 @@ class KvCache:
         step, dev = self._current_step(), self.device
         T, w = step.T, self.q_width
         with _On(dev):
-            out = torch.empty((T, w), dtype=torch.bfloat16, device=dev) if out is None else out
+            out = _like(q, T, w, dev) if out is None else out
             B.lora_kv_attend(self.kv, layer, step.raw, self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(),
                              _rows(q, T, w, dev, "q"), _rows(out, T, w, dev, "out"), _stream_of(stream, self.device))
         return out
@@ -553,7 +560,8 @@ class KvCache:
         """Keys and values of the tokens (seq[i], position[i]) as the bf16 values that their codes stand for."""
         n, dev = len(seq), self.device
         with _On(dev):
-            k, v = (torch.empty((n, self.k_width), dtype=torch.bfloat16, device=dev) for _ in range(2))
+            k = torch.empty((n, self.k_width), dtype=torch.bfloat16, device=dev)
+            v = torch.empty_like(k)
             if n:
                 B.lora_kv_read(self.kv, layer, n, _ints(seq, n, dev, "seq"), _ints(position, n, dev, "position"), k.data_ptr(), v.data_ptr(),
                                _stream_of(stream, self.device))
