@@ -455,8 +455,8 @@ lora_status lora_priority_sorting(int32_t n_adapters, const int32_t *size, const
  * previous call's is ordered behind it with an event.  While a stream is being captured no event is recorded or waited
  * for, and replays are outside the library: the caller orders a capture and each of its replays with the other calls
  * on that cache (two graphs of one cache must not run at the same time).  A captured call reads the lengths, rows and
- * tables that are there when it is replayed, but keeps T, n and max_new of the capture; rows of the step behind a
- * captured T are left alone.
+ * tables that are there when it is replayed, but keeps T, n and max_new of the capture: the step in force at a replay is
+ * one of the same three (requests without new tokens and rows behind the last request make a smaller one).
  * ------------------------------------------------------------------------------------------------------------- */
 #define LORA_KV_BLOCK 64
 
@@ -508,7 +508,7 @@ size_t lora_kv_slab_bytes(const lora_kv_config *cfg);
  * head_dim), OOM (slab too small), HIP. */
 lora_status lora_kv_create(const lora_kv_config *cfg, lora_kv **out);
 
-/* Waits for the device and ends the cache; the slab stays the caller's.  Errors: INVALID_ARG (NULL). */
+/* Waits for the cache's device and ends the cache; the slab stays the caller's.  Errors: INVALID_ARG (NULL). */
 lora_status lora_kv_destroy(lora_kv *kv);
 
 /* Blocks and places for the new tokens of a step (paper Sec. 2.1: prompts' tokens and one-token requests run in one

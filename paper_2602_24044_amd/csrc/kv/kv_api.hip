@@ -242,8 +242,12 @@ lora_status lora_kv_destroy(lora_kv* k)
 {
     if (!k) return LORA_ERR_INVALID_ARG;
     if (k->ev) {
+        int dev = -1;
+        (void)hipGetDevice(&dev);
+        if (dev != k->device) (void)hipSetDevice(k->device);
         (void)hipDeviceSynchronize();
         (void)hipEventDestroy(k->ev);
+        if (dev >= 0 && dev != k->device) (void)hipSetDevice(dev);
     }
     delete k;
     return LORA_OK;

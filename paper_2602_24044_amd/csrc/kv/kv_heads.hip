@@ -4,12 +4,13 @@
 //   u = x / sqrt(mean(x^2) + eps) * w            (where there is a weight)
 //   y_p = u_p cos a - u_p' sin a,  y_p' = u_p' cos a + u_p sin a,   a = position * f_p,  p' = p + D/2 (or its neighbour)
 //
-// One read and one write of every head, so the copy rate bounds it: 4099 tokens of 32 + 8 heads of 128 with norm, 67 MB, in 17.8 us (3.8
-// TB/s), 8190 into the cache, 313 MB with the queries, in 74 (4.2 TB/s: the keys' double arithmetic and the codes keep the vector
-// unit busy for two thirds of it), out of it 16.5.  D / 8 lanes share a head's row, 16 bytes each; the other half of
-// a rotated pair sits D / 16 lanes away.  Angles are taken in 64 bits (a far position times a frequency has few bits left behind the
-// point in 32) once per token and pair, and shared by all heads through LDS.  Keys on the way to four bits are computed in 64 bits
-// throughout and rounded to 32 once: next to a border between two codes an error of 2^-24 would pick the wrong one now and then.
+// One read and one write of every head, so the copy rate bounds it: 4099 tokens of 28 + 4 heads of 128 with norm, 67 MB, in 17.8 us (3.8
+// TB/s); 8190 tokens of 64 + 8 heads with norm into the cache, 313 MB, in 74 us (4.2 TB/s: the keys' double arithmetic and the codes
+// keep the vector unit busy for two thirds of it), and their keys and values out of it in 16.5.  D / 8 lanes share a head's row, 16
+// bytes each; the other half of a rotated pair sits D / 16 lanes away.  Angles are taken in 64 bits (a far position times a frequency
+// has few bits left behind the point in 32) once per token and pair, and shared by all heads through LDS.  Keys on the way to four bits
+// are computed in 64 bits throughout and rounded to 32 once: next to a border between two codes an error of 2^-24 would pick the wrong
+// one now and then.
 #include "kv_device.hpp"
 
 #include <algorithm>
