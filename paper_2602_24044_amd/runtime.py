@@ -315,7 +315,7 @@ class ModelSession:
         if self.w.proj[q][1] != cache.q_width or self.w.proj[k][1] != cache.k_width or self.w.proj[v][1] != cache.k_width:
             raise ValueError("the cache's heads are not those of the q, k and v projections")
         if self._heads is None:
-            self._heads = [torch.empty((self.w.T, cache.q_width), dtype=torch.bfloat16, device=self.device) for _ in range(2)]
+            self._heads = [_made(stream, (self.w.T, cache.q_width), self.device) for _ in range(2)]
         rotated, mixed = self._heads
         s = (stream or torch.cuda.current_stream()).cuda_stream
         out = self.out[l]
@@ -370,11 +370,19 @@ def _stream_of(stream: Optional[torch.cuda.Stream], device: torch.device) -> int
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
 
-def _like(t: torch.Tensor, rows: int, width: int, device) -> torch.Tensor:
+def _made(stream: Optional[torch.cuda.Stream], shape, device) -> torch.Tensor:
+    """An output, out of the memory of the stream that will write it: another stream's may still have work on it."""
+    if stream is None:
+        return torch.empty(shape, dtype=torch.bfloat16, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=torch.bfloat16, device=device)
+
+
+def _like(t: torch.Tensor, rows: int, width: int, stream: Optional[torch.cuda.Stream], device) -> torch.Tensor:
     """An output [rows, width] beside the operand t.  (Shorter for the host where t itself is dense.)"""
-    if t.is_contiguous() and t.shape == (rows, width):
+    if stream is None and t.is_contiguous() and t.shape == (rows, width):
         return torch.empty_like(t)
-    return torch.empty((rows, width), dtype=torch.bfloat16, device=device)
+    return _made(stream, (rows, width), device)
 
 
 def _rows(t: torch.Tensor, rows: int, width: int, device, what: str) -> int:
@@ -429,11 +437,11 @@ def head_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], n_hea
     with _On(device):
         at = {"q": (None, 0), "k": (None, 0), "q_out": (None, 0), "k_out": (None, 0)}
         if q is not None:
-            q_out = _like(q, T, n_heads * dim, device) if q_out is None else q_out
+            q_out = _like(q, T, n_heads * dim, stream, device) if q_out is None else q_out
             at["q"] = q.data_ptr(), _rows(q, T, n_heads * dim, device, "q")
             at["q_out"] = q_out.data_ptr(), _rows(q_out, T, n_heads * dim, device, "q_out")
         if k is not None:
-            k_out = _like(k, T, n_kv_heads * dim, device) if k_out is None else k_out
+            k_out = _like(k, T, n_kv_heads * dim, stream, device) if k_out is None else k_out
             at["k"] = k.data_ptr(), _rows(k, T, n_kv_heads * dim, device, "k")
             at["k_out"] = k_out.data_ptr(), _rows(k_out, T, n_kv_heads * dim, device, "k_out")
         h = _heads(dim, device, inv_freq, q_norm, k_norm, eps, pairing, **at)
@@ -538,7 +546,7 @@ class KvCache:
         with _On(dev):
             at = {"k": (k.data_ptr(), _rows(k, T, self.k_width, dev, "k")), "v": (v.data_ptr(), _rows(v, T, self.k_width, dev, "v"))}
             if q is not None:
-                out = _like(q, T, self.q_width, dev) if out is None else out
+                out = _like(q, T, self.q_width, stream, dev) if out is None else out
                 at["q"] = q.data_ptr(), _rows(q, T, self.q_width, dev, "q")
                 at["q_out"] = out.data_ptr(), _rows(out, T, self.q_width, dev, "out")
             h = _heads(self.head_dim, dev, inv_freq, q_norm, k_norm, eps, pairing, **at)
@@ -551,7 +559,7 @@ class KvCache:
         step, dev = self._current_step(), self.device
         T, w = step.T, self.q_width
         with _On(dev):
-            out = _like(q, T, w, dev) if out is None else out
+            out = _like(q, T, w, stream, dev) if out is None else out
             B.lora_kv_attend(self.kv, layer, step.raw, self.head_dim ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(),
                              _rows(q, T, w, dev, "q"), _rows(out, T, w, dev, "out"), _stream_of(stream, self.device))
         return out
@@ -560,8 +568,7 @@ class KvCache:
         """Keys and values of the tokens (seq[i], position[i]) as the bf16 values that their codes stand for."""
         n, dev = len(seq), self.device
         with _On(dev):
-            k = torch.empty((n, self.k_width), dtype=torch.bfloat16, device=dev)
-            v = torch.empty_like(k)
+            k, v = (_made(stream, (n, self.k_width), dev) for _ in range(2))
             if n:
                 B.lora_kv_read(self.kv, layer, n, _ints(seq, n, dev, "seq"), _ints(position, n, dev, "position"), k.data_ptr(), v.data_ptr(),
                                _stream_of(stream, self.device))

@@ -7,7 +7,7 @@ import torch
 import oracle.kv as okv
 from kv_util import Model, announce, attend_bound, bf16, f64, i32
 from paper_2602_24044_amd import binding as B
-from paper_2602_24044_amd.runtime import KvCache, rotary_inv_freq
+from paper_2602_24044_amd.runtime import KvCache, head_norm_rotate, rotary_inv_freq
 
 # (its bound: the queries' norm and rotation are fp32 sums, so a pair's difference is off relative to the pair)
 from test_gpu_kv_heads import _check as heads_check  # noqa: E402
@@ -152,6 +152,34 @@ def test_calls_on_other_streams_wait_for_each_other():
     finally:
         m.close()
         p.close()
+
+
+def test_outputs_come_from_the_stream_that_writes_them():
+    """Memory given back on the current stream, which still has a write to it in its queue, is not an output of another stream."""
+    m = Model(8, 2, 64, n_blocks=20, max_seqs=2, max_seq_tokens=512, max_tokens=256)
+    side = torch.cuda.Stream()
+    try:
+        m.extend([0], [0], [200])
+        m.store(0)
+        q, k, v = (bf16(m.rng, 200, w).cuda() for w in (512, 128, 128))
+        position, row = i32(range(200)), i32([0] * 200)
+        calls = [lambda s: m.kv.attend(0, q, stream=s), lambda s: head_norm_rotate(q, k, 8, 2, None, stream=s)[0],
+                 lambda s: head_norm_rotate(q, k, 8, 2, None, stream=s)[1], lambda s: m.kv.read(0, row, position, stream=s)[0],
+                 lambda s: m.kv.store(0, k, v, q=q, stream=s)]
+        for call in calls:
+            want = call(None).clone()
+            torch.cuda.synchronize()
+            held = [torch.empty_like(want) for _ in range(4)]
+            torch.cuda.synchronize()
+            torch.cuda._sleep(20_000_000)                      # some milliseconds
+            for t in held:
+                t.fill_(7.0)
+            del held, t
+            got = call(side)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+    finally:
+        m.close()
 
 
 def test_steps_of_nothing():
