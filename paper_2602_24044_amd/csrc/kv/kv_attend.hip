@@ -414,11 +414,12 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 // registers, where each thread converts an eighth of 16 tokens to bf16 operands of V^T in LDS, once for all four waves.  Two stages: the next
 // block is made while this one is used.
 //
-// A prompt of 8192 tokens, 32 heads on 8 of 128 (550 GFLOP) takes 500 - 550 us: 1.0 - 1.1 PFLOP/s, where a large bf16 product reaches 1.25.
+// A prompt of 8192 tokens, 32 heads on 8 of 128 (550 GFLOP) takes 490 - 550 us: 1.0 - 1.1 PFLOP/s, where a large bf16 product reaches 1.25.
 // Matrix and vector units are busy for half of the time each and LDS for as much; leaving out any one of them (scores, exponentials,
 // conversion, products with the values) takes 5 - 17 % off, so it is the chain through all of them, twice on each SIMD, that counts.
 // Not kept: 64 columns a wave, alone on its SIMD (694 us: scores and sums change places between the two kinds of registers);
-// conversion and maximum between the products with the values (557); the conversion's lanes dealt out otherwise (570).
+// conversion and maximum between the products with the values (545 - 563, with and without priorities); the conversion's lanes dealt
+// out otherwise (570).
 //
 // Values, as the 256 threads load them: a chunk of four tokens, kE dimensions.  That is half of an operand of V^T for each of these: the
 // other half are the four tokens eight further.
@@ -606,6 +607,9 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
         // The order is pinned here: an MFMA of the next scores (of no use in the last iteration: what is in LDS then are older codes), and in
         // its time a part of this block's weights on the vector unit; values from LDS a group of operands ahead of the MFMAs that want
         // them.  Left to itself the compiler asks LDS for an operand right in front of each MFMA.
+        // Priority over the SIMD's other wave from here on, whose conversion and maximum fill what the matrix units leave (8192 tokens: 565 ->
+        // 547 us, 1900 behind 6100 268 -> 253; for the products with the values alone 570 and 268, the other way round 557 and 256).
+        __builtin_amdgcn_s_setprio(1);
         Keys keys;
         read_keys(keys, ahead);
         s_next[0] = s_next[1] = zero;
@@ -639,6 +643,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
             for (int d = 0; d < N; ++d) o[d] = mfma32(as_bf16x8(f[u & 1][d]), as_bf16x8(w[u]), o[d]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         landed<0>();
     };
     f32x16 s_other[2];
