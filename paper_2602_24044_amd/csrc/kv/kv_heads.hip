@@ -95,80 +95,70 @@ __device__ inline double reciprocal_root(double x)
     return y;
 }
 
-// What a lane needs for every row of a token: cos and sin of its pairs, and with a norm the weights of its values and of those of the lane that
-// has their partners.  R = float (queries, and keys that stay bf16) or double (keys on their way to four bits).
-template <int D, typename R> struct Turn {
-    R c[8], s[8];
+// What the rows of a token share: y = (x a + x' b) / rms for every value x and its partner x', a = w cos and b = -+ w' sin with the weights
+// of the norm in them (the angle's sine with the sign that the value's place in its pair has).  In LDS in the order in which lanes read: 16
+// bytes each, lanes side by side.  R = float (queries, and keys that stay bf16) or double (keys on their way to four bits).
+template <typename R> struct Pair {
+    R a, b;
 };
-template <typename R> struct Weights {
-    bool on;
-    R own[8], other[8];
-};
-template <int D, typename R> __device__ inline void load_weights(Weights<R>& w, const uint16_t* p)
+template <int D, typename R> __device__ inline int pair_at(int d)
 {
-    constexpr int L = D / 8;
-    const int l = threadIdx.x % L;
-    w.on = p != nullptr;
-    if (!w.on) return;
-    const u32x4 a = load16(p + 8 * l), b = load16(p + 8 * (l ^ (L / 2)));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        w.own[2 * j] = (R)lo_f32(a[j]);
-        w.own[2 * j + 1] = (R)hi_f32(a[j]);
-        w.other[2 * j] = (R)lo_f32(b[j]);
-        w.other[2 * j + 1] = (R)hi_f32(b[j]);
-    }
+    constexpr int L = D / 8, per = sizeof(R) == 4 ? 2 : 1;
+    return ((d % 8) / per * L + d / 8) * per + d % per;
 }
-template <int D, typename R> __device__ inline void load_turn(Turn<D, R>& t, const double2* cs, bool pairs)
-{
-    const int l = threadIdx.x % (D / 8);
-    // halves: pair p = (8 l + j) % (D / 2), and the second half takes the sine with its own sign; neighbours: pair 4 l + j / 2
+template <int D, typename R> struct Turn {
+    Pair<R> p[8];
+    __device__ void load(const Pair<R>* of, int l)
+    {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const double2 v = cs[pairs ? 4 * l + j / 2 : (8 * l + j) % (D / 2)];
-        t.c[j] = (R)v.x;
-        t.s[j] = (R)((pairs ? (j & 1) : l >= D / 16) ? v.y : -v.y);
+        for (int j = 0; j < 8; ++j) p[j] = of[pair_at<D, R>(8 * l + j)];
     }
+};
+
+__device__ inline double bf16_at(const uint16_t* w, int d) { return w ? (double)__builtin_bit_cast(float, (uint32_t)w[d] << 16) : 1.0; }
+
+// The two values of pair k, which turns by the angle of (sine, cosine).
+template <int D, typename R> __device__ inline void put_pair(Pair<R>* to, int k, bool pairs, double sine, double cosine, const uint16_t* w)
+{
+    const int d0 = pairs ? 2 * k : k, d1 = pairs ? 2 * k + 1 : k + D / 2;
+    const double w0 = bf16_at(w, d0), w1 = bf16_at(w, d1);
+    to[pair_at<D, R>(d0)] = Pair<R>{(R)(cosine * w0), (R)(-sine * w1)};
+    to[pair_at<D, R>(d1)] = Pair<R>{(R)(cosine * w1), (R)(sine * w0)};
 }
 
 // Norm and rotation of one row of D values, eight of them in a lane.
 template <int D, typename R>
-__device__ inline void norm_rotate(const u32x4 raw, const Weights<R>& w, float eps, const Turn<D, R>& t, bool rotate, bool pairs, R (&y)[8])
+__device__ inline void norm_rotate(const u32x4 raw, bool norm, float eps, const Turn<D, R>& t, bool rotate, bool pairs, R (&y)[8])
 {
     constexpr int L = D / 8;
-    R x[8], inv = 1;
+    R x[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         x[2 * j] = (R)lo_f32(raw[j]);
         x[2 * j + 1] = (R)hi_f32(raw[j]);
     }
-    if (w.on) {
-        R sum = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
-        inv = reciprocal_root(row_sum<L>(sum) * (R)(1.0 / D) + (R)eps);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= inv * w.own[j];
-    }
     if (!rotate) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = x[j];
+        for (int j = 0; j < 8; ++j) y[j] = norm ? x[j] * t.p[j].a : x[j];
     } else if (pairs) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = x[j] * t.c[j] + x[j ^ 1] * t.s[j];
+        for (int j = 0; j < 8; ++j) y[j] = x[j] * t.p[j].a + x[j ^ 1] * t.p[j].b;
     } else {
-        // the partners as they were read (half the exchange), with their own weights
+        // the partners as they were read (half the exchange)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t o = across<L>(raw[j]);
-            R a = (R)lo_f32(o), b = (R)hi_f32(o);
-            if (w.on) {
-                a *= inv * w.other[2 * j];
-                b *= inv * w.other[2 * j + 1];
-            }
-            y[2 * j] = x[2 * j] * t.c[2 * j] + a * t.s[2 * j];
-            y[2 * j + 1] = x[2 * j + 1] * t.c[2 * j + 1] + b * t.s[2 * j + 1];
+            y[2 * j] = x[2 * j] * t.p[2 * j].a + (R)lo_f32(o) * t.p[2 * j].b;
+            y[2 * j + 1] = x[2 * j + 1] * t.p[2 * j + 1].a + (R)hi_f32(o) * t.p[2 * j + 1].b;
         }
+    }
+    if (norm) {
+        R sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += x[j] * x[j];
+        const R inv = reciprocal_root(row_sum<L>(sum) * (R)(1.0 / D) + (R)eps);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] *= inv;
     }
 }
 
@@ -210,31 +200,32 @@ template <int D> __device__ inline uint32_t get_v(const uint8_t* part, int k, in
 // end in the cache, keys and values of a token side by side.
 template <int D, int TPW, bool CACHE> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
 {
+    using K = std::conditional_t<CACHE, double, float>;
     constexpr int L = D / 8, ROWS = 256 / L, P = D / 2, U = 4;
-    __shared__ double2 cs[TPW][P];
+    __shared__ __align__(16) Pair<float> q_pairs[TPW][D];
+    __shared__ __align__(16) Pair<K> k_pairs[TPW][D];
     const int t0 = blockIdx.x * TPW;
     const int T = CACHE ? min(a.T, a.head->rows) : a.T;
     if (t0 >= T) return;
     const int count = min(TPW, T - t0);
     const bool rotate = a.inv_freq != nullptr;
     const int l = threadIdx.x % L, group = threadIdx.x / L;
-    if (rotate) {
+    if (rotate || a.q_norm || a.k_norm) {
         for (int k = threadIdx.x; k < count * P; k += 256) {
-            double s, c;
-            sin_cos((double)a.position[t0 + k / P] * (double)a.inv_freq[k % P], s, c);
-            cs[k / P][k % P] = double2{c, s};
+            double s = 0.0, c = 1.0;
+            if (rotate) sin_cos((double)a.position[t0 + k / P] * (double)a.inv_freq[k % P], s, c);
+            if (a.q) put_pair<D, float>(q_pairs[k / P], k % P, a.pairs, s, c, a.q_norm);
+            if (a.k) put_pair<D, K>(k_pairs[k / P], k % P, a.pairs, s, c, a.k_norm);
         }
         __syncthreads();
     }
 
-    auto dense = [&](const uint16_t* in, int64_t in_stride, uint16_t* out, int64_t out_stride, const uint16_t* weight, int heads) {
-        Weights<float> w;
-        load_weights<D>(w, weight);
+    auto dense = [&](const uint16_t* in, int64_t in_stride, uint16_t* out, int64_t out_stride, const Pair<float> (*shared)[D], bool norm, int heads) {
         for (int tt = 0; tt < count; ++tt) {
             const size_t t = t0 + tt;
             const bool kept = !CACHE || a.slot[t] >= 0;
             Turn<D, float> turn;
-            if (rotate) load_turn<D>(turn, cs[tt], a.pairs);
+            if (rotate || norm) turn.load(shared[tt], l);
             const uint16_t* from = in + t * in_stride + 8 * l;
             uint16_t* to = out + t * out_stride + 8 * l;
             for (int h0 = group; h0 < heads; h0 += U * ROWS) {
@@ -246,7 +237,7 @@ template <int D, int TPW, bool CACHE> __global__ __launch_bounds__(256) void hea
                 for (int u = 0; u < U; ++u) {
                     if (h0 + u * ROWS >= heads) continue;
                     float y[8];
-                    norm_rotate<D, float>(raw[u], w, a.eps, turn, rotate, a.pairs, y);
+                    norm_rotate<D, float>(raw[u], norm, a.eps, turn, rotate, a.pairs, y);
                     u32x4 o;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[j] = kept ? pack_bf16(y[2 * j], y[2 * j + 1]) : 0u;
@@ -255,49 +246,46 @@ template <int D, int TPW, bool CACHE> __global__ __launch_bounds__(256) void hea
             }
         }
     };
-    if (a.q) dense(a.q, a.q_stride, a.q_out, a.q_out_stride, a.q_norm, a.n_heads);
+    if (a.q) dense(a.q, a.q_stride, a.q_out, a.q_out_stride, q_pairs, a.q_norm, a.n_heads);
     if constexpr (!CACHE) {
-        if (a.k) dense(a.k, a.k_stride, a.k_out, a.k_out_stride, a.k_norm, a.n_kv);
-        return;
-    }
-
-    Weights<double> w;
-    load_weights<D>(w, a.k_norm);
-    bool odd = false;
-    const int per = 2 * a.n_kv;
-    for (int r = group; r < count * per; r += ROWS) {
-        const int tt = r / per, h = r - tt * per;
-        const size_t t = t0 + tt;
-        const bool is_k = h < a.n_kv;
-        const int hk = is_k ? h : h - a.n_kv;
-        const int slot = a.slot[t];                    // (all lanes of a row agree on what follows)
-        if (slot < 0) continue;
-        float v[8];
-        const u32x4 raw = load16((is_k ? a.k + t * a.k_stride : a.v + t * a.v_stride) + (size_t)hk * D + 8 * l);
-        if (is_k) {
-            Turn<D, double> turn;
-            double y[8];
-            if (rotate) load_turn<D>(turn, cs[tt], a.pairs);
-            norm_rotate<D, double>(raw, w, a.eps, turn, rotate, a.pairs, y);
+        if (a.k) dense(a.k, a.k_stride, a.k_out, a.k_out_stride, k_pairs, a.k_norm, a.n_kv);
+    } else {
+        bool odd = false;
+        const int per = 2 * a.n_kv;
+        for (int r = group; r < count * per; r += ROWS) {
+            const int tt = r / per, h = r - tt * per;
+            const size_t t = t0 + tt;
+            const bool is_k = h < a.n_kv;
+            const int hk = is_k ? h : h - a.n_kv;
+            const int slot = a.slot[t];                    // (all lanes of a row agree on what follows)
+            if (slot < 0) continue;
+            float v[8];
+            const u32x4 raw = load16((is_k ? a.k + t * a.k_stride : a.v + t * a.v_stride) + (size_t)hk * D + 8 * l);
+            if (is_k) {
+                Turn<D, double> turn;
+                double y[8];
+                if (rotate || a.k_norm) turn.load(k_pairs[tt], l);
+                norm_rotate<D, double>(raw, a.k_norm, a.eps, turn, rotate, a.pairs, y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (float)y[j];
-        } else {
+                for (int j = 0; j < 8; ++j) v[j] = (float)y[j];
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[2 * j] = lo_f32(raw[j]);
-                v[2 * j + 1] = hi_f32(raw[j]);
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] = lo_f32(raw[j]);
+                    v[2 * j + 1] = hi_f32(raw[j]);
+                }
             }
+            int exponent;
+            const uint32_t codes = to_codes(v, exponent, odd);
+            uint8_t* part = a.cache + ((size_t)(slot / kBlock) * a.n_kv + hk) * Part<D>::kBytes;
+            const int k = slot % kBlock;
+            if (is_k) *reinterpret_cast<uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l) = codes;
+            else put_v<D>(part, k, l, codes);
+            if (l % 4 == 0)
+                part[is_k ? Part<D>::kKExp + Part<D>::k_exp_at(k, l / 4) : Part<D>::kVExp + Part<D>::v_exp_at(k, l / 4)] = (uint8_t)exponent;
         }
-        int exponent;
-        const uint32_t codes = to_codes(v, exponent, odd);
-        uint8_t* part = a.cache + ((size_t)(slot / kBlock) * a.n_kv + hk) * Part<D>::kBytes;
-        const int k = slot % kBlock;
-        if (is_k) *reinterpret_cast<uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l) = codes;
-        else put_v<D>(part, k, l, codes);
-        if (l % 4 == 0)
-            part[is_k ? Part<D>::kKExp + Part<D>::k_exp_at(k, l / 4) : Part<D>::kVExp + Part<D>::v_exp_at(k, l / 4)] = (uint8_t)exponent;
+        if (odd) atomicOr(&a.head->flags, kFlagNotFinite);
     }
-    if (odd) atomicOr(&a.head->flags, kFlagNotFinite);
 }
 
 template <int D> __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
