@@ -4,13 +4,12 @@
 //   u = x / sqrt(mean(x^2) + eps) * w            (where there is a weight)
 //   y_p = u_p cos a - u_p' sin a,  y_p' = u_p' cos a + u_p sin a,   a = position * f_p,  p' = p + D/2 (or its neighbour)
 //
-// One read and one write of every head, so the copy rate bounds it: 4099 tokens of 28 + 4 heads of 128 with norm, 67 MB, in 17.8 us (3.8
-// TB/s); 8190 tokens of 64 + 8 heads with norm into the cache, 313 MB, in 74 us (4.2 TB/s: the keys' double arithmetic and the codes
-// keep the vector unit busy for two thirds of it), and their keys and values out of it in 16.5.  D / 8 lanes share a head's row, 16
-// bytes each; the other half of a rotated pair sits D / 16 lanes away.  Angles are taken in 64 bits (a far position times a frequency
-// has few bits left behind the point in 32) once per token and pair, and shared by all heads through LDS.  Keys on the way to four bits
-// are computed in 64 bits throughout and rounded to 32 once: next to a border between two codes an error of 2^-24 would pick the wrong
-// one now and then.
+// One read and one write of every head, so the copy rate bounds it: 4099 tokens of 28 + 4 heads of 128 with norm, 67 MB, in 14.9 us (4.5
+// TB/s); 8190 tokens of 64 + 8 heads with norm into the cache, 313 MB, in 67 us (4.7 TB/s; the vector unit is busy for half of it), and
+// their keys and values out of it in 16.5.  D / 8 lanes share a head's row, 16 bytes each; the other half of a rotated pair sits D / 16
+// lanes away.  Angles are taken in 64 bits (a far position times a frequency has few bits left behind the point in 32) once per token and
+// pair, and shared by all heads through LDS.  Keys on the way to four bits are computed in 64 bits throughout and rounded to 32 once: next
+// to a border between two codes an error of 2^-24 would pick the wrong one now and then.
 #include "kv_device.hpp"
 
 #include <algorithm>
@@ -196,53 +195,59 @@ template <int D> __device__ inline uint32_t get_v(const uint8_t* part, int k, in
            (uint32_t)*reinterpret_cast<const uint16_t*>(v + Part<D>::v_at(k, 8 * l + 4)) << 16;
 }
 
-// A workgroup takes TPW tokens.  Rows of queries (and of keys that stay bf16) go through its lane groups four at a time, then those that
-// end in the cache, keys and values of a token side by side.
-template <int D, int TPW, bool CACHE> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
+// A workgroup takes a token: rows of queries (and of keys that stay bf16) go through its lane groups four at a time, then those that
+// end in the cache, keys and values side by side.  (Four tokens a workgroup: 25.4 us instead of 25.2 for the rotation of 4096 tokens of 32 + 8
+// heads out of HBM, 16.2 instead of 14.1 for 2048; into the cache 33.4 instead of 36.6, but 21.8 instead of 20.0.)
+template <int D, bool CACHE> __global__ __launch_bounds__(256) void heads_kernel(HeadsArgs a)
 {
     using K = std::conditional_t<CACHE, double, float>;
-    constexpr int L = D / 8, ROWS = 256 / L, P = D / 2, U = 4;
-    __shared__ __align__(16) Pair<float> q_pairs[TPW][D];
-    __shared__ __align__(16) Pair<K> k_pairs[TPW][D];
-    const int t0 = blockIdx.x * TPW;
-    const int T = CACHE ? min(a.T, a.head->rows) : a.T;
-    if (t0 >= T) return;
-    const int count = min(TPW, T - t0);
+    constexpr int L = D / 8, ROWS = 256 / L, U = 4, KV = 2;
+    __shared__ __align__(16) Pair<float> q_pairs[D];
+    __shared__ __align__(16) Pair<K> k_pairs[D];
+    const size_t t = blockIdx.x;
+    if (CACHE && (int)t >= a.head->rows) return;
     const bool rotate = a.inv_freq != nullptr;
     const int l = threadIdx.x % L, group = threadIdx.x / L;
+    const int slot = CACHE ? a.slot[t] : 0;
+    // The first rows on their way to the cache are asked for in front of everything else.
+    u32x4 rows[KV];
+    auto fetch = [&](int from) {
+#pragma unroll
+        for (int u = 0; u < KV; ++u) {
+            const int h = from + u * ROWS;
+            if (h < 2 * a.n_kv) rows[u] = load16((h < a.n_kv ? a.k + t * a.k_stride + (size_t)h * D : a.v + t * a.v_stride + (size_t)(h - a.n_kv) * D) + 8 * l);
+        }
+    };
+    if constexpr (CACHE) fetch(group);
     if (rotate || a.q_norm || a.k_norm) {
-        for (int k = threadIdx.x; k < count * P; k += 256) {
+        for (int k = threadIdx.x; k < D / 2; k += 256) {
             double s = 0.0, c = 1.0;
-            if (rotate) sin_cos((double)a.position[t0 + k / P] * (double)a.inv_freq[k % P], s, c);
-            if (a.q) put_pair<D, float>(q_pairs[k / P], k % P, a.pairs, s, c, a.q_norm);
-            if (a.k) put_pair<D, K>(k_pairs[k / P], k % P, a.pairs, s, c, a.k_norm);
+            if (rotate) sin_cos((double)a.position[t] * (double)a.inv_freq[k], s, c);
+            if (a.q) put_pair<D, float>(q_pairs, k, a.pairs, s, c, a.q_norm);
+            if (a.k) put_pair<D, K>(k_pairs, k, a.pairs, s, c, a.k_norm);
         }
         __syncthreads();
     }
 
-    auto dense = [&](const uint16_t* in, int64_t in_stride, uint16_t* out, int64_t out_stride, const Pair<float> (*shared)[D], bool norm, int heads) {
-        for (int tt = 0; tt < count; ++tt) {
-            const size_t t = t0 + tt;
-            const bool kept = !CACHE || a.slot[t] >= 0;
-            Turn<D, float> turn;
-            if (rotate || norm) turn.load(shared[tt], l);
-            const uint16_t* from = in + t * in_stride + 8 * l;
-            uint16_t* to = out + t * out_stride + 8 * l;
-            for (int h0 = group; h0 < heads; h0 += U * ROWS) {
-                u32x4 raw[U];
+    auto dense = [&](const uint16_t* in, int64_t in_stride, uint16_t* out, int64_t out_stride, const Pair<float>* shared, bool norm, int heads) {
+        Turn<D, float> turn;
+        if (rotate || norm) turn.load(shared, l);
+        const uint16_t* from = in + t * in_stride + 8 * l;
+        uint16_t* to = out + t * out_stride + 8 * l;
+        for (int h0 = group; h0 < heads; h0 += U * ROWS) {
+            u32x4 raw[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (h0 + u * ROWS < heads) raw[u] = load16(from + (size_t)(h0 + u * ROWS) * D);
+            for (int u = 0; u < U; ++u)
+                if (h0 + u * ROWS < heads) raw[u] = load16(from + (size_t)(h0 + u * ROWS) * D);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (h0 + u * ROWS >= heads) continue;
-                    float y[8];
-                    norm_rotate<D, float>(raw[u], norm, a.eps, turn, rotate, a.pairs, y);
-                    u32x4 o;
+            for (int u = 0; u < U; ++u) {
+                if (h0 + u * ROWS >= heads) continue;
+                float y[8];
+                norm_rotate<D, float>(raw[u], norm, a.eps, turn, rotate, a.pairs, y);
+                u32x4 o;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = kept ? pack_bf16(y[2 * j], y[2 * j + 1]) : 0u;
-                    *reinterpret_cast<u32x4*>(to + (size_t)(h0 + u * ROWS) * D) = o;
-                }
+                for (int j = 0; j < 4; ++j) o[j] = slot >= 0 ? pack_bf16(y[2 * j], y[2 * j + 1]) : 0u;
+                *reinterpret_cast<u32x4*>(to + (size_t)(h0 + u * ROWS) * D) = o;
             }
         }
     };
@@ -250,39 +255,40 @@ template <int D, int TPW, bool CACHE> __global__ __launch_bounds__(256) void hea
     if constexpr (!CACHE) {
         if (a.k) dense(a.k, a.k_stride, a.k_out, a.k_out_stride, k_pairs, a.k_norm, a.n_kv);
     } else {
+        if (slot < 0) return;                          // a refused request's
         bool odd = false;
-        const int per = 2 * a.n_kv;
-        for (int r = group; r < count * per; r += ROWS) {
-            const int tt = r / per, h = r - tt * per;
-            const size_t t = t0 + tt;
-            const bool is_k = h < a.n_kv;
-            const int hk = is_k ? h : h - a.n_kv;
-            const int slot = a.slot[t];                    // (all lanes of a row agree on what follows)
-            if (slot < 0) continue;
-            float v[8];
-            const u32x4 raw = load16((is_k ? a.k + t * a.k_stride : a.v + t * a.v_stride) + (size_t)hk * D + 8 * l);
-            if (is_k) {
-                Turn<D, double> turn;
-                double y[8];
-                if (rotate || a.k_norm) turn.load(k_pairs[tt], l);
-                norm_rotate<D, double>(raw, a.k_norm, a.eps, turn, rotate, a.pairs, y);
+        Turn<D, double> turn;
+        if (rotate || a.k_norm) turn.load(k_pairs, l);
+        for (int from = group; from < 2 * a.n_kv; from += KV * ROWS) {
+            if (from != group) fetch(from);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = (float)y[j];
-            } else {
+            for (int u = 0; u < KV; ++u) {
+                const int h = from + u * ROWS;
+                if (h >= 2 * a.n_kv) continue;
+                const bool is_k = h < a.n_kv;
+                const int hk = is_k ? h : h - a.n_kv;
+                float v[8];
+                if (is_k) {
+                    double y[8];
+                    norm_rotate<D, double>(rows[u], a.k_norm, a.eps, turn, rotate, a.pairs, y);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[2 * j] = lo_f32(raw[j]);
-                    v[2 * j + 1] = hi_f32(raw[j]);
+                    for (int j = 0; j < 8; ++j) v[j] = (float)y[j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v[2 * j] = lo_f32(rows[u][j]);
+                        v[2 * j + 1] = hi_f32(rows[u][j]);
+                    }
                 }
+                int exponent;
+                const uint32_t codes = to_codes(v, exponent, odd);
+                uint8_t* part = a.cache + ((size_t)(slot / kBlock) * a.n_kv + hk) * Part<D>::kBytes;
+                const int k = slot % kBlock;
+                if (is_k) *reinterpret_cast<uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l) = codes;
+                else put_v<D>(part, k, l, codes);
+                if (l % 4 == 0)
+                    part[is_k ? Part<D>::kKExp + Part<D>::k_exp_at(k, l / 4) : Part<D>::kVExp + Part<D>::v_exp_at(k, l / 4)] = (uint8_t)exponent;
             }
-            int exponent;
-            const uint32_t codes = to_codes(v, exponent, odd);
-            uint8_t* part = a.cache + ((size_t)(slot / kBlock) * a.n_kv + hk) * Part<D>::kBytes;
-            const int k = slot % kBlock;
-            if (is_k) *reinterpret_cast<uint32_t*>(part + Part<D>::kK + k * Part<D>::kRow + 4 * l) = codes;
-            else put_v<D>(part, k, l, codes);
-            if (l % 4 == 0)
-                part[is_k ? Part<D>::kKExp + Part<D>::k_exp_at(k, l / 4) : Part<D>::kVExp + Part<D>::v_exp_at(k, l / 4)] = (uint8_t)exponent;
         }
         if (odd) atomicOr(&a.head->flags, kFlagNotFinite);
     }
@@ -318,17 +324,8 @@ template <int D> __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 
 template <int D> hipError_t heads(const HeadsArgs& a, hipStream_t stream)
 {
-    // A token of its own per workgroup, or four, whose angles keep all threads busy and whose norm weights are loaded once.  One / four,
-    // 32 + 8 heads of 128 out of HBM: rotation of 256 tokens 6.4 / 13.2 us, 2048 17.0 / 18.3, 4096 28.1 / 26.8; into the cache 2048
-    // tokens 21.7 / 23.8, 8192 76 / 71.
-    const int wgs = a.T <= 2048 ? a.T : (a.T + 3) / 4;
-    if (a.cache) {
-        if (a.T <= 2048) heads_kernel<D, 1, true><<<wgs, 256, 0, stream>>>(a);
-        else heads_kernel<D, 4, true><<<wgs, 256, 0, stream>>>(a);
-    } else {
-        if (a.T <= 2048) heads_kernel<D, 1, false><<<wgs, 256, 0, stream>>>(a);
-        else heads_kernel<D, 4, false><<<wgs, 256, 0, stream>>>(a);
-    }
+    if (a.cache) heads_kernel<D, true><<<a.T, 256, 0, stream>>>(a);
+    else heads_kernel<D, false><<<a.T, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 template <int D> hipError_t read(const ReadArgs& a, hipStream_t stream)
