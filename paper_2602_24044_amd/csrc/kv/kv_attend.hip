@@ -678,9 +678,12 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 
 // The partial results of tiles that were cut along their keys, in one pass with a running maximum.  D / 4 lanes take a column, four
 // dimensions each; the groups of lanes of a workgroup have a column each, or share the pieces of one where there are many.
-template <int D> __global__ __launch_bounds__(256) void merge_kernel(AttendArgs a)
+// Nearly all of it is waiting for the pieces, which other CUs have just written: 256 pieces of 32 columns take 6.8 us, of which 4.6 are an empty
+// launch's (with 256 threads, half the groups, 8.8; with 1024 8.2; eight pieces' requests at once instead of four: no less).
+constexpr int kMergeThreads = 512;
+template <int D> __global__ __launch_bounds__(kMergeThreads) void merge_kernel(AttendArgs a)
 {
-    constexpr int L = D / 4, GROUPS = 256 / L;
+    constexpr int L = D / 4, GROUPS = kMergeThreads / L;
     __shared__ float sAcc[GROUPS][D], sM[GROUPS], sL[GROUPS];
     const int tid = threadIdx.x, lane = tid % L, group = tid / L;
     for (int item = blockIdx.x; item < a.n_merge * a.n_kv; item += gridDim.x) {
@@ -732,7 +735,7 @@ template <int D> hipError_t attend(const AttendArgs& a, int n, int n_cus, hipStr
     // columns at most; more pieces than that go round)
     const long few = std::min<long>(a.n_few, (long)n * (kFewMost / kFewCols) + kFewItems / a.n_kv + 1);
     attend_few_kernel<D><<<(unsigned)std::min<long>(few * a.n_kv, 1 << 20), 64, 0, stream>>>(a);
-    merge_kernel<D><<<(unsigned)std::min<long>((long)a.n_merge * a.n_kv, 4L * n_cus), 256, 0, stream>>>(a);
+    merge_kernel<D><<<(unsigned)std::min<long>((long)a.n_merge * a.n_kv, 4L * n_cus), kMergeThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -94,9 +94,9 @@ struct Entry {
 };
 static_assert(sizeof(Entry) == 64, "one line");
 // Columns whose tile's range was split: the partial results are merged behind.  kMergeCols columns an entry, or one where there are at least
-// kMergeMany pieces (all lanes of a workgroup then work on it: 8 requests of 32 pieces 4.8 us, 7.9 with eight columns an entry; with four
-// pieces and more it is the same either way).
-constexpr int kMergeCols = 8, kMergeMany = 16;
+// kMergeMany pieces (all lanes of a workgroup then work on it: 8 requests of 32 pieces 4.8 us, 7.9 without that; from four pieces on
+// it is the same either way).
+constexpr int kMergeCols = 16, kMergeMany = 16;
 struct Merge {
     int32_t first, rows;   // as in Entry
     int32_t col, cols; // first column, and how many
