@@ -30,7 +30,9 @@ constexpr int kFewMost = 64;
 // eleven waves a CU find room, 256 requests of mixed lengths take 86 - 90 us with 2048 pieces and more with 1536 or 2816 - 6144.  Many
 // columns, 256 / 512 / 1024 pieces: 500 tokens behind 16000 178 / 160 / 172 us, 2000 tokens alone 60 / 60 / 70, and a merge of 7 / 9 / 12.
 constexpr int kFewItems = 2048, kManyItems = 512;
-constexpr int kFewChunk = 4, kManyChunk = 8;   // blocks of the smallest piece
+// Blocks of the smallest piece.  (Few columns, 2 / 3 / 4: one request of 2000 tokens 6.9 / 8.0 / 9.1 us, 8 of 1000 9.0 / 9.6 / 10.3, 32 of 700
+// 14.9 / 14.5 / 14.5.)
+constexpr int kFewChunk = 2, kManyChunk = 8;
 constexpr int kMinExp = -100, kMaxExp = 125;
 
 // Bits of the device flag word (LORA_KV_FLAG_*).

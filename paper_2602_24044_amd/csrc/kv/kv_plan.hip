@@ -79,7 +79,7 @@ __device__ inline unsigned long long cut_columns(Request& q, int group)
 __device__ inline int piece_blocks(unsigned long long work, int n_kv, int items, int least)
 {
     const unsigned long long per = (work * n_kv + items - 1) / items;
-    return ((int)(per < (unsigned)least ? least : per > kMaxBlocks ? kMaxBlocks : per) + 3) & ~3;
+    return ((int)(per < (unsigned)least ? least : per > kMaxBlocks ? kMaxBlocks : per) + 1) & ~1;
 }
 __device__ inline int merge_columns(const Request& q) { return q.splits < kMergeMany ? kMergeCols : 1; }
 // v: entries (few, many), partial results (few, many), merges of the request.  A tile of few columns is cut into pieces of `chunk` blocks at

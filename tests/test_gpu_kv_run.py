@@ -254,7 +254,7 @@ def test_columns_on_both_sides_of_a_tile(heads, kv, past, new):
         m.close()
 
 
-@pytest.mark.parametrize("blocks", [4, 5, 8, 9, 60, 61, 64, 65])
+@pytest.mark.parametrize("blocks", [2, 3, 4, 5, 8, 9, 30, 31, 32, 33, 60, 61, 64, 65])
 @pytest.mark.parametrize("new", [1, 50])
 def test_pieces_of_one_sequence(blocks, new):
     """Sequences of so many blocks that they just make another piece, and as many pieces as are merged another way."""
