@@ -415,7 +415,7 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 // block is made while this one is used.
 //
 // A prompt of 8192 tokens, 32 heads on 8 of 128 (550 GFLOP) takes 490 - 550 us: 1.0 - 1.1 PFLOP/s, where a large bf16 product reaches 1.25.
-// Matrix and vector units are busy for half of the time each and LDS for as much; leaving out any one of them (scores, exponentials,
+// Matrix and vector units are busy for half of the time each, LDS for a third; leaving out any one of them (scores, exponentials,
 // conversion, products with the values) takes 5 - 17 % off, so it is the chain through all of them, twice on each SIMD, that counts.
 // Not kept: 64 columns a wave, alone on its SIMD (694 us: scores and sums change places between the two kinds of registers);
 // conversion and maximum between the products with the values (545 - 563, with and without priorities); the conversion's lanes dealt
