@@ -390,7 +390,7 @@ def _rows(t: torch.Tensor, rows: int, width: int, device, what: str) -> int:
     if t.dtype is not torch.bfloat16 or t.device != device or t.shape != (rows, width):
         raise ValueError(f"{what}: bf16 [{rows}, {width}] on {device} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
     stride, one = t.stride()
-    if one != 1 or (rows > 1 and stride < width):
+    if rows and (one != 1 or (rows > 1 and stride < width)):      # (strides of a tensor without elements say nothing)
         raise ValueError(f"{what}: the values of a row must lie next to each other, and rows must not overlap")
     return stride if rows > 1 else width
 

@@ -97,3 +97,25 @@ def test_cache_bytes():
     assert r["four_bits"] == 2 * 26112 and 26112 * 8 == 2 * 3 * 2 * 64 * 64 * 4.25
     assert r["bf16"] == 65 * 2 * 3 * 2 * 64 * 2
     assert r["tokens_per_slot"] == 128                   # whole blocks
+
+
+def test_operand_checks():
+    """What the Python layer takes as rows of bf16 and as integers (no GPU needed for it)."""
+    import numpy as np
+    import torch
+
+    from paper_2602_24044_amd.runtime import _ints, _rows
+    cpu = torch.device("cpu")
+    x = torch.zeros((6, 128), dtype=torch.bfloat16)
+    assert _rows(x, 6, 128, cpu, "x") == 128 and _rows(x[:, :64], 6, 64, cpu, "x") == 128 and _rows(x[::2], 3, 128, cpu, "x") == 256
+    assert _rows(x[:1], 1, 128, cpu, "x") == 128
+    empty = torch.from_numpy(np.zeros((0, 128), dtype=np.float32)).bfloat16()
+    assert empty.stride() == (0, 0) and _rows(empty, 0, 128, cpu, "x") == 128 and _rows(x[:0], 0, 128, cpu, "x") == 128
+    for bad, width in ((x.float(), 128), (x[:5], 128), (x[:, :64], 128), (x[:, ::2], 64), (x[:1].expand(6, 128), 128), (x[0], 128)):
+        with pytest.raises(ValueError):
+            _rows(bad, 6, width, cpu, "x")
+    n = torch.arange(6, dtype=torch.int32)
+    assert _ints(n, 6, cpu, "n") == n.data_ptr()
+    for bad in (n.long(), n[:5], torch.arange(12, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError):
+            _ints(bad, 6, cpu, "n")
