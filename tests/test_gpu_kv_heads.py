@@ -112,6 +112,24 @@ def test_store_and_read(heads, kv, dim, norm, neighbours):
         m.close()
 
 
+@pytest.mark.parametrize("heads,kv,dim", [(40, 20, 128), (17, 17, 128), (80, 40, 64), (300, 100, 64)])
+@pytest.mark.parametrize("k_norm", [False, True])
+def test_store_of_many_key_heads(heads, kv, dim, k_norm):
+    """More rows on their way to the cache than a workgroup asks for at once; a norm of the keys alone."""
+    m = Model(heads, kv, dim, n_blocks=4, max_seqs=2, max_seq_tokens=128, max_tokens=8, seed=kv)
+    try:
+        m.extend([1], [0], [3])
+        freq = rotary_inv_freq(dim, 10000.0, "cuda:0")
+        weight = bf16(m.rng, dim).cuda() if k_norm else None
+        q = bf16(m.rng, 3, heads * dim).cuda()
+        out = m.store(0, bf16(m.rng, 3, kv * dim), bf16(m.rng, 3, kv * dim), q=q, inv_freq=freq, k_norm=weight)
+        _check(out, q, None, 1e-6, np.arange(3), freq, False, heads)
+        ko, vo = m.kv.read(0, i32([1] * 3), i32(range(3)))
+        assert np.array_equal(f64(ko).reshape(3, kv, dim), m.keys[0][1]) and np.array_equal(f64(vo).reshape(3, kv, dim), m.values[0][1])
+    finally:
+        m.close()
+
+
 def test_store_of_borders_extremes_and_what_is_not_finite():
     m = Model(2, 1, 128, n_blocks=4, max_seqs=2, max_seq_tokens=128, max_tokens=128)
     try:
