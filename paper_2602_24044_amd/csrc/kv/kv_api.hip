@@ -70,7 +70,7 @@ Layout make_layout(const lora_kv_config* c)
     const size_t few = (size_t)most_few(T, seqs, (int)group, n_kv), many = (size_t)most_many(T, seqs, (int)group, n_kv);
     // (and one that says that the list has ended)
     L.few = take(sizeof(Entry) * (few + 1));
-    L.many = take(sizeof(Entry) * (many + 1));
+    L.many = take(sizeof(Entry) * many);
     L.merge = take(sizeof(Merge) * (T * group + 1));
     // a cut tile has a partial result per piece, and its pieces are at least half of what a cut is aimed at; nor are there more than the
     // smallest pieces make
@@ -359,7 +359,8 @@ lora_status lora_kv_attend(lora_kv* k, int32_t layer, const lora_kv_step* step, 
     a.n_few = (int)few;
     a.n_many = (int)many;
     a.n_merge = step->T * a.group;
-    return KV_HIP_FAIL(launch_attend(a, k->cfg.head_dim, step->n, k->n_cus, s)) ? LORA_ERR_HIP : LORA_OK;
+    a.n_cus = k->n_cus;
+    return KV_HIP_FAIL(launch_attend(a, k->cfg.head_dim, step->n, s)) ? LORA_ERR_HIP : LORA_OK;
 }
 
 lora_status lora_kv_read(lora_kv* k, int32_t layer, int32_t n, const int32_t* d_seq, const int32_t* d_position, void* d_k_out, void* d_v_out,

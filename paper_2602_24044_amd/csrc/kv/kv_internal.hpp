@@ -178,6 +178,7 @@ struct AttendArgs {
     float scale_log2;                   // scale * log2(e)
     int32_t T, n_kv, group;
     int32_t n_few, n_many, n_merge;     // entries that the lists can have (n_many 0: none)
+    int32_t n_cus;
 };
 
 hipError_t launch_plan(const PlanArgs& a, hipStream_t stream);
@@ -185,7 +186,7 @@ hipError_t launch_release(const Tables& t, int n, const int32_t* seq, const int3
 hipError_t launch_heads(const HeadsArgs& a, int dim, hipStream_t stream);
 hipError_t launch_read(const ReadArgs& a, int dim, hipStream_t stream);
 // n: requests of the step
-hipError_t launch_attend(const AttendArgs& a, int dim, int n, int n_cus, hipStream_t stream);
+hipError_t launch_attend(const AttendArgs& a, int dim, int n, hipStream_t stream);
 
 }  // namespace kv
 }  // namespace lora

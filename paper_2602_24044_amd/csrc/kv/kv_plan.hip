@@ -96,12 +96,11 @@ __device__ inline void cut_keys(Request& q, int group, int chunk_few, int chunk_
     v[3] = q.splits > 1 ? v[1] : 0;
     v[4] = q.splits > 1 ? (q.rows * group + together - 1) / together : 0;
 }
-// Ends the lists behind their entries: what the step before had there is no longer any.
+// Ends the lists behind their entries: what the step before had there is no longer any.  (The kernel of many columns reads how many there are.)
 template <int THREADS> __device__ inline void end_lists(const Tables& t, int few, int many, int merge)
 {
     const int tid = threadIdx.x;
     for (int k = few + tid; k < t.head->n_few; k += THREADS) t.few[k].rows = 0;
-    for (int k = many + tid; k < t.head->n_many; k += THREADS) t.many[k].rows = 0;
     for (int k = merge + tid; k < t.head->n_merge; k += THREADS) t.merge[k].rows = 0;
     __syncthreads();
     if (tid == 0) {
