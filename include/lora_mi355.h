@@ -503,8 +503,8 @@ typedef struct {
  * n_kv_heads * 68 * head_dim bytes: 4.25 bits a value. */
 size_t lora_kv_slab_bytes(const lora_kv_config *cfg);
 
-/* Creates an empty cache on the current device (paper Sec. 2.1).  Sets the whole cache to zero and waits for it.
- * Calls on one cache are not thread-safe.  Errors: INVALID_ARG (null, out of range, misaligned slab), SHAPE (heads,
+/* Creates an empty cache on the current device (paper Sec. 2.1).  Waits for the device (the slab may come from a use whose
+ * last work is still queued), sets the whole cache to zero and waits for that.  Calls on one cache are not thread-safe.  Errors: INVALID_ARG (null, out of range, misaligned slab), SHAPE (heads,
  * head_dim), OOM (slab too small), HIP. */
 lora_status lora_kv_create(const lora_kv_config *cfg, lora_kv **out);
 

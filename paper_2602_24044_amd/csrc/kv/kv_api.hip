@@ -225,8 +225,9 @@ lora_status lora_kv_create(const lora_kv_config* cfg, lora_kv** out)
     bool ok = !KV_HIP_FAIL(hipGetDevice(&k->device)) && !KV_HIP_FAIL(hipEventCreateWithFlags(&k->ev, hipEventDisableTiming));
     if (ok) {
         k->n_cus = compute_units();
-        // everything starts at zero: stale codes and exponents stand for finite numbers from the start
-        ok = !KV_HIP_FAIL(launch_fill_i32(k->at<int32_t>(0), 0, k->L.total / 4, nullptr)) &&
+        // everything starts at zero: stale codes and exponents stand for finite numbers from the start.  (The memory may be fresh from
+        // another use whose last write is still in a stream's queue, which the fills do not wait for by themselves.)
+        ok = !KV_HIP_FAIL(hipDeviceSynchronize()) && !KV_HIP_FAIL(launch_fill_i32(k->at<int32_t>(0), 0, k->L.total / 4, nullptr)) &&
              !KV_HIP_FAIL(launch_fill_i32(k->at<int32_t>(k->L.table), -1, (size_t)cfg->max_seqs * row_blocks_of(cfg), nullptr)) &&
              !KV_HIP_FAIL(hipDeviceSynchronize());
     }

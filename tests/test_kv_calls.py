@@ -1,0 +1,43 @@
+"""What the calls of the cache in four bits ask of the runtime, and in which order, and what a failure leaves behind: the host side
+linked with a runtime that writes its calls down (tests/sanitize/kv_driver.cpp), under AddressSanitizer and UndefinedBehaviorSanitizer."""
+import os
+import subprocess
+
+import pytest
+
+from paper_2602_24044_amd import binding as B
+from test_sanitizers import SAN, run_clean
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("kv_calls") / "kv_driver")
+    subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=all", "-fno-omit-frame-pointer", os.path.join(SAN, "kv_driver.cpp"), "-o", exe], check=True)
+
+    def run(*script):
+        """One line per call: (status, the runtime calls it made)."""
+        lines = run_clean([exe], stdin="\n".join(script) + "\n").splitlines()
+        return [(int(line.split()[1]), line.split()[2:]) for line in lines]
+    return run
+
+
+def test_calls_of_a_step(driver):
+    assert driver("create", "extend 1 5", "store 1 0", "attend 1 0", "read 1", "poll 1", "release 1", "store 1 0")[1:] == [
+        (0, ["plan1"]), (0, ["heads1"]), (0, ["attend1"]), (0, ["read1"]), (0, ["copy", "fill", "stream_wait1"]), (0, ["release1"]),
+        (B.LORA_ERR_INVALID_ARG, [])]
+
+
+def test_another_stream_waits(driver):
+    assert driver("create", "extend 1 5", "store 2 0", "attend 2 0", "poll 0")[1:] == [
+        (0, ["plan1"]), (0, ["record1", "wait2", "heads2"]), (0, ["attend2"]), (0, ["record2", "wait0", "copy", "fill", "stream_wait0"])]
+
+
+def test_a_captured_call_records_and_waits_for_nothing(driver):
+    assert driver("create", "extend 1 5", "capture 2 1", "extend 2 5", "store 2 0", "capture 2 0", "attend 1 0")[1:] == [
+        (0, ["plan1"]), (0, ["plan2"]), (0, ["heads2"]), (0, ["attend1"])]
+
+
+def test_create_waits_for_the_device_around_its_fills(driver):
+    """The memory may still have a write of its last owner in a queue, on a stream that the fills' does not wait for."""
+    assert driver("create") == [(0, ["device_wait", "fill", "fill", "device_wait"])]
