@@ -454,7 +454,8 @@ lora_status lora_priority_sorting(int32_t n_adapters, const int32_t *size, const
  * Streams.  Calls on one cache share its tables and scratch.  As with a lora_ctx, a call whose stream differs from the
  * previous call's is ordered behind it with an event.  While a stream is being captured no event is recorded or waited
  * for, and replays are outside the library: the caller orders a capture and each of its replays with the other calls
- * on that cache (two graphs of one cache must not run at the same time).  A captured call reads the lengths, rows and
+ * on that cache (two graphs of one cache must not run at the same time).  While the stream of the latest call made outside of a
+ * capture is being captured, a call on another stream that is not cannot wait for it: INVALID_ARG.  A captured call reads the lengths, rows and
  * tables that are there when it is replayed, but keeps T, n and max_new of the capture: the step in force at a replay is
  * one of the same three (requests without new tokens and rows behind the last request make a smaller one).
  * ------------------------------------------------------------------------------------------------------------- */

@@ -178,7 +178,8 @@ struct lora_kv {
     }
 
     // Called in front of every launch: the cache's device must be current, and a stream other than the previous call's waits for
-    // that call, unless it is being captured (see the header).
+    // that call, unless it is being captured (see the header).  Where the previous call's is, an event recorded on it would draw the
+    // other stream into the capture: such a call is refused.
     lora_status enter(hipStream_t s)
     {
         int dev = -1;
@@ -188,6 +189,9 @@ struct lora_kv {
         if (KV_HIP_FAIL(hipStreamIsCapturing(s, &cs))) return LORA_ERR_HIP;
         if (cs != hipStreamCaptureStatusNone) return LORA_OK;
         if (have_last && last != s) {
+            // (the default stream is never captured, and asking about it is an error while others are)
+            if (last && KV_HIP_FAIL(hipStreamIsCapturing(last, &cs))) return LORA_ERR_HIP;
+            if (cs != hipStreamCaptureStatusNone) return LORA_ERR_INVALID_ARG;
             if (KV_HIP_FAIL(hipEventRecord(ev, last)) || KV_HIP_FAIL(hipStreamWaitEvent(s, ev, 0))) return LORA_ERR_HIP;
         }
         last = s;

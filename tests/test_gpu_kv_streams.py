@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from kv_util import Model
+from kv_util import Model, bf16
 from paper_2602_24044_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -34,5 +34,38 @@ def test_cache_made_on_a_stream_with_a_write_queued():
         m.store(0)
         m.check_attend(0)
         assert m.kv.poll() == (B.LORA_OK, 0)
+    finally:
+        m.close()
+
+
+def test_a_call_on_another_stream_inside_a_capture_is_refused():
+    """The capture stays what it is: it ends, and its replays give what the eager call gives."""
+    m = Model(**SHAPE)
+    try:
+        m.fill([2], [90])
+        m.extend([2], [90], [7])
+        m.store(0)
+        q = bf16(m.rng, 7, 256)
+        want = m.check_attend(0, q=q).clone()
+        dq, out, other = q.cuda(), torch.zeros_like(want), torch.full_like(want, 3.0)
+        side, third = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        m.kv.attend(0, dq, out=out, stream=side)               # the latest call outside of a capture
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            m.kv.attend(0, dq, out=out, stream=side)
+            with pytest.raises(B.LoraError) as e:
+                m.kv.attend(0, dq, out=other, stream=third)
+        assert e.value.status == B.LORA_ERR_INVALID_ARG
+        for _ in range(3):
+            out.zero_()
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and (other == 3.0).all()
+        m.kv.attend(0, dq, out=other, stream=third)
+        torch.cuda.synchronize()
+        assert torch.equal(other, want) and m.kv.poll() == (B.LORA_OK, 0)
     finally:
         m.close()

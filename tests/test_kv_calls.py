@@ -41,3 +41,15 @@ def test_a_captured_call_records_and_waits_for_nothing(driver):
 def test_create_waits_for_the_device_around_its_fills(driver):
     """The memory may still have a write of its last owner in a queue, on a stream that the fills' does not wait for."""
     assert driver("create") == [(0, ["device_wait", "fill", "fill", "device_wait"])]
+
+
+def test_no_event_goes_into_a_capture(driver):
+    """A call on another stream while the previous call's is being captured: there is no way to wait for that one's work, so the call is
+    refused and nothing is enqueued.  Calls on the captured stream go on, and the other's once the capture has ended."""
+    out = driver("create", "extend 1 5", "capture 1 1", "store 1 0", "store 2 0", "poll 2", "attend 1 0", "capture 1 0", "attend 2 0")
+    assert out[1:] == [(0, ["plan1"]), (0, ["heads1"]), (B.LORA_ERR_INVALID_ARG, []), (B.LORA_ERR_INVALID_ARG, []), (0, ["attend1"]),
+                       (0, ["record1", "wait2", "attend2"])]
+    # the same with a release and a read, and a new step, which leaves the one before it in force
+    out = driver("create", "extend 1 5", "capture 1 1", "extend 2 5", "release 2", "read 2", "capture 1 0", "attend 1 0")
+    assert out[1:] == [(0, ["plan1"]), (B.LORA_ERR_INVALID_ARG, []), (B.LORA_ERR_INVALID_ARG, []), (B.LORA_ERR_INVALID_ARG, []),
+                       (0, ["attend1"])]
