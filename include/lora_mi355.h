@@ -525,14 +525,15 @@ lora_status lora_kv_destroy(lora_kv *kv);
  * sequence would exceed max_seq_tokens, d_len is not covered by blocks that the row holds, or its rows do not fit T.  Free
  * blocks are handed out in order until a request does not get all that it needs: it and all later requests that
  * need one get none and are refused (LORA_KV_FLAG_EXHAUSTED).
- * Errors: INVALID_ARG (n or T out of range, max_new < 0, null pointers), HIP. */
+ * Errors: INVALID_ARG (n or T out of range, max_new < 0, null pointers), HIP (a launch that fails ends the step before: blocks that
+ * were on their way to a request may then be lost to the pool). */
 lora_status lora_kv_extend(lora_kv *kv, int32_t n, const int32_t *d_seq, const int32_t *d_len, const int32_t *d_new, int32_t T,
                            int32_t max_new, lora_kv_step *out, void *stream);
 
 /* Gives the blocks of n rows back to the pool, apart from those that hold the first d_keep[i] tokens (d_keep NULL: none are
  * kept; a sequence that has ended, or proposed tokens that were rejected).  The same row may be named more than
  * once.  A row that does not exist or a negative d_keep sets LORA_KV_FLAG_REFUSED and changes nothing.  The step of
- * the latest lora_kv_extend ends with it.  Errors: INVALID_ARG, HIP. */
+ * the latest lora_kv_extend ends with it, also where a launch fails.  Errors: INVALID_ARG, HIP. */
 lora_status lora_kv_release(lora_kv *kv, int32_t n, const int32_t *d_seq, const int32_t *d_keep, void *stream);
 
 /* Operands of the norm and rotation of heads.  Everything is bf16 with the values of a head next to each other and the

@@ -198,6 +198,12 @@ struct lora_kv {
         have_last = true;
         return LORA_OK;
     }
+    // In front of the launches that change the tables: where one of them fails, others may have run.
+    void end_step()
+    {
+        ++epoch;
+        step_n = step_T = -1;
+    }
     bool current(const lora_kv_step* st) const
     {
         return st && step_n >= 0 && st->epoch == epoch && st->n == step_n && st->T == step_T;
@@ -276,6 +282,7 @@ lora_status lora_kv_extend(lora_kv* k, int32_t n, const int32_t* d_seq, const in
     a.n_kv = k->cfg.n_kv_heads;
     a.group = k->cfg.n_heads / k->cfg.n_kv_heads;
     a.whole = 0;
+    k->end_step();
     if (KV_HIP_FAIL(launch_plan(a, s))) return LORA_ERR_HIP;
     k->step_n = n;
     k->step_T = T;
@@ -288,7 +295,7 @@ lora_status lora_kv_extend(lora_kv* k, int32_t n, const int32_t* d_seq, const in
     out->row_blocks = a.t.row_blocks;
     out->n = n;
     out->T = T;
-    out->epoch = ++k->epoch;
+    out->epoch = k->epoch;
     return LORA_OK;
 }
 
@@ -297,10 +304,8 @@ lora_status lora_kv_release(lora_kv* k, int32_t n, const int32_t* d_seq, const i
     if (!k || n < 0 || (n > 0 && (!d_seq || misaligned(d_seq, 4))) || misaligned(d_keep, 4)) return LORA_ERR_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (const lora_status st = k->enter(s); st != LORA_OK) return st;
-    if (KV_HIP_FAIL(launch_release(k->tables(), n, d_seq, d_keep, s))) return LORA_ERR_HIP;
-    ++k->epoch;
-    k->step_n = k->step_T = -1;
-    return LORA_OK;
+    k->end_step();
+    return KV_HIP_FAIL(launch_release(k->tables(), n, d_seq, d_keep, s)) ? LORA_ERR_HIP : LORA_OK;
 }
 
 lora_status lora_head_norm_rotate(int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t* d_position,

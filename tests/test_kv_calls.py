@@ -53,3 +53,17 @@ def test_no_event_goes_into_a_capture(driver):
     out = driver("create", "extend 1 5", "capture 1 1", "extend 2 5", "release 2", "read 2", "capture 1 0", "attend 1 0")
     assert out[1:] == [(0, ["plan1"]), (B.LORA_ERR_INVALID_ARG, []), (B.LORA_ERR_INVALID_ARG, []), (B.LORA_ERR_INVALID_ARG, []),
                        (0, ["attend1"])]
+
+
+@pytest.mark.parametrize("call,launch", [("extend 1 5", "plan1!"), ("release 1", "release1!")])
+def test_a_step_ends_with_a_call_that_failed_on_the_way(driver, call, launch):
+    """A launch that fails may have others behind it that ran: the step before is no longer what the tables say."""
+    out = driver("create", "extend 1 7", "store 1 0", "fail " + launch[:-2], call, "store 1 0", "attend 1 0", "extend 1 5", "store 1 1",
+                 "store 1 0")
+    refused = (B.LORA_ERR_INVALID_ARG, [])
+    assert out[1:] == [(0, ["plan1"]), (0, ["heads1"]), (B.LORA_ERR_HIP, [launch]), refused, refused, (0, ["plan1"]), refused, (0, ["heads1"])]
+
+
+def test_a_step_outlives_a_call_that_was_refused(driver):
+    out = driver("create", "extend 1 7", "extend 1 101", "extend 1 -1", "store 1 0")
+    assert [r[0] for r in out[1:]] == [0, B.LORA_ERR_INVALID_ARG, B.LORA_ERR_INVALID_ARG, 0]
