@@ -212,7 +212,7 @@ lora_status lora_bucket(lora_ctx *ctx, const int32_t *d_token_adapter, int32_t T
  * Stream ordering: all forward calls (and segment maps) of one context share its scratch (split-K partial tiles,
  * shrink results, the counters of a launch), so they must not overlap in time.  The library sees to that itself:
  * a call whose stream differs from the stream of the context's previous lora_bucket / forward call is ordered
- * behind it with an event before anything is enqueued.  Calls that should run concurrently need contexts of
+ * behind it with an event before anything is enqueued (the previous call's stream has to exist then).  Calls that should run concurrently need contexts of
  * their own.  When the call uses the shrink inside its launch and lora_poll_device_flags later reports
  * LORA_FLAG_INTERNAL, the outputs written since the previous poll are undefined.
  * Errors: INVALID_ARG (proj out of range, stale seg, null or misaligned pointers), HIP. */
@@ -452,7 +452,8 @@ lora_status lora_priority_sorting(int32_t n_adapters, const int32_t *size, const
  * that a query does not see.
  *
  * Streams.  Calls on one cache share its tables and scratch.  As with a lora_ctx, a call whose stream differs from the
- * previous call's is ordered behind it with an event.  While a stream is being captured no event is recorded or waited
+ * previous call's is ordered behind it with an event, which is recorded then: the previous call's stream has to live until
+ * the next call (or until lora_kv_destroy).  While a stream is being captured no event is recorded or waited
  * for, and replays are outside the library: the caller orders a capture and each of its replays with the other calls
  * on that cache (two graphs of one cache must not run at the same time).  While the stream of the latest call made outside of a
  * capture is being captured, a call on another stream that is not cannot wait for it: INVALID_ARG.  A captured call reads the lengths, rows and

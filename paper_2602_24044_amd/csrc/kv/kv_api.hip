@@ -190,9 +190,11 @@ struct lora_kv {
         if (cs != hipStreamCaptureStatusNone) return LORA_OK;
         if (have_last && last != s) {
             // (the default stream is never captured, and asking about it is an error while others are)
-            if (last && KV_HIP_FAIL(hipStreamIsCapturing(last, &cs))) return LORA_ERR_HIP;
+            bool ordered = !last || !KV_HIP_FAIL(hipStreamIsCapturing(last, &cs));
             if (cs != hipStreamCaptureStatusNone) return LORA_ERR_INVALID_ARG;
-            if (KV_HIP_FAIL(hipEventRecord(ev, last)) || KV_HIP_FAIL(hipStreamWaitEvent(s, ev, 0))) return LORA_ERR_HIP;
+            ordered = ordered && !KV_HIP_FAIL(hipEventRecord(ev, last)) && !KV_HIP_FAIL(hipStreamWaitEvent(s, ev, 0));
+            // (its stream is gone, against the header: the device's work is waited for, and later calls do not meet it again)
+            if (!ordered && KV_HIP_FAIL(hipDeviceSynchronize())) return LORA_ERR_HIP;
         }
         last = s;
         have_last = true;

@@ -67,3 +67,18 @@ def test_a_step_ends_with_a_call_that_failed_on_the_way(driver, call, launch):
 def test_a_step_outlives_a_call_that_was_refused(driver):
     out = driver("create", "extend 1 7", "extend 1 101", "extend 1 -1", "store 1 0")
     assert [r[0] for r in out[1:]] == [0, B.LORA_ERR_INVALID_ARG, B.LORA_ERR_INVALID_ARG, 0]
+
+
+def test_a_stream_that_is_gone_holds_up_one_call_at_most(driver):
+    """The header wants the latest call's stream alive.  Where the runtime says that it is not, its work is waited for with the device, and
+    the calls go on."""
+    out = driver("create", "extend 1 5", "end 1", "store 2 0", "attend 2 0", "poll 3")
+    assert out[1:] == [(0, ["plan1"]), (0, ["device_wait", "heads2"]), (0, ["attend2"]),
+                       (0, ["record2", "wait3", "copy", "fill", "stream_wait3"])]
+    # an event that cannot be recorded, or not be waited for
+    for name, calls in (("record", ["record1!", "device_wait", "heads2"]), ("wait", ["record1", "wait2!", "device_wait", "heads2"])):
+        out = driver("create", "extend 1 5", f"fail {name}", "store 2 0", "attend 1 0")
+        assert out[2:] == [(0, calls), (0, ["record2", "wait1", "attend1"])]
+    # a wait that fails too, and a new stream that is not one, are errors; nothing is forgotten
+    out = driver("create", "extend 1 5", "end 1", "fail device_wait", "store 2 0", "store 2 0", "end 4", "store 4 0", "store 2 0")
+    assert out[1:] == [(0, ["plan1"]), (B.LORA_ERR_HIP, ["device_wait!"]), (0, ["device_wait", "heads2"]), (B.LORA_ERR_HIP, []), (0, ["heads2"])]
