@@ -541,8 +541,9 @@ lora_status lora_kv_release(lora_kv *kv, int32_t n, const int32_t *d_seq, const 
  * heads of a token next to each other; strides count elements from token to token (0: dense; multiples of 8, at
  * least the heads' width), pointers are 16-byte aligned.  Norm (where there is a weight): u = x / sqrt(mean(x^2) + eps) * w over
  * each head.  Rotation (where d_inv_freq is given): the pair p = 0 .. head_dim / 2 - 1 turns by the angle position *
- * d_inv_freq[p], taken in 64 bits.  Sums and products are fp32 (of keys on their way into a cache fp64: a row of queries whose
- * squares' sum leaves fp32's range comes out as zeros or NaN); one rounding of the result. */
+ * d_inv_freq[p], taken in 64 bits.  Sums and products are fp32 (of keys on their way into a cache fp64), of rows with a norm whose
+ * mean square lies outside of 2^-40 .. 2^40 on values scaled by a power of two, so that rows of any finite values have the norm that the
+ * formula gives them (zeros without an eps: NaN); one rounding of the result. */
 typedef struct {
     const void *d_q, *d_k, *d_v;
     int64_t q_stride, k_stride, v_stride;
