@@ -577,8 +577,8 @@ lora_status lora_kv_store(lora_kv *kv, int32_t layer, const lora_kv_step *step, 
  * keys k <= position[t] of the token's sequence (its own among them: lora_kv_store comes first).  d_q: bf16 [T, n_heads *
  * head_dim], normed and rotated; d_out: the same shape, apart from d_q; strides as in lora_heads.  Keys and values enter as the exact
  * values that their codes stand for; a query's values as bf16 has them, but those below 2^-14 of the head's largest, which may be
- * off by 2^-21 of it.  Scores and sums are fp32 (a score or a sum of values beyond its range gives a NaN or an infinity in its
- * head); the weights of the softmax are rounded to bf16, and it is these that their sum counts; one rounding of the result.  A
+ * off by 2^-21 of it.  Scores and sums are fp32 (a score above its range, all of a query's scores below it, or a sum of
+ * values beyond it gives a NaN or an infinity in its head); the weights of the softmax are rounded to bf16, and it is these that their sum counts; one rounding of the result.  A
  * NaN or an infinity in a query makes its own head's row NaN.  Rows of a refused request are set to zero, rows behind the last
  * request are left as they are.  The result does not depend on what else the step holds beyond these roundings, and is the
  * same from call to call.

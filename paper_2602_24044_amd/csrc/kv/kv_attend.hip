@@ -397,7 +397,8 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
                 a.few_ml[slot * 2 + 1] = l;
             }
         } else {
-            const float f = l == 0.f ? 0.f : 1.0f / l;              // no key at all: a refused request, its rows are zero
+            // (no block: a refused request, its rows are zero.  No weight behind keys: every score lies below the range, 0 / 0)
+            const float f = n == 0 ? 0.f : 1.0f / l;
             uint16_t* o = a.out + (size_t)(r.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + quad * (D / 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -669,7 +670,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
             a.many_ml[slot * 2 + 1] = l;
         }
     } else {
-        const float f = l == 0.f ? 0.f : 1.0f / l;
+        const float f = 1.0f / l;                      // (a column sees its own key at least)
         uint16_t* out = a.out + (size_t)(e.first + token) * a.out_stride + ((size_t)hk * a.group + head) * D + 4 * h;
 #pragma unroll
         for (int d = 0; d < N; ++d)
@@ -725,7 +726,7 @@ template <int D> __global__ __launch_bounds__(kMergeThreads) void merge_kernel(A
 #pragma unroll
                 for (int w = 1; w < GROUPS; ++w) add(sM[w], sL[w], *reinterpret_cast<const f32x4*>(&sAcc[w][4 * lane]));
             }
-            const float f = l == 0.f ? 0.f : 1.0f / l;
+            const float f = 1.0f / l;                      // (no weight at all: every score lies below the range, 0 / 0)
             uint16_t* o = a.out + (size_t)(g.first + token) * a.out_stride + ((size_t)h * a.group + head) * D + 4 * lane;
             *reinterpret_cast<u32x2*>(o) = u32x2{pack_bf16(acc[0] * f, acc[1] * f), pack_bf16(acc[2] * f, acc[3] * f)};
         }

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import oracle.kv as okv
-from kv_util import Model, announce, bf16, f64, i32
+import oracle.kv as okv
+from kv_util import Model, announce, attend_bound, bf16, f64, i32
 from paper_2602_24044_amd import binding as B
 from paper_2602_24044_amd.runtime import head_norm_rotate, rotary_inv_freq
 from test_gpu_kv_heads import _check as heads_check
@@ -62,5 +63,69 @@ def test_stored_queries_at_every_scale():
         keep[0, 5] = keep[1, 70] = keep[2, 9] = False
         assert torch.equal(got[keep.cuda()], out.view(3, heads, dim)[keep.cuda()])
         assert m.kv.poll() == (B.LORA_OK, 0)
+    finally:
+        m.close()
+
+
+@pytest.mark.parametrize("heads,kv,dim,past,new", [(8, 2, 64, 0, 1), (8, 2, 128, 70, 3), (4, 1, 128, 3000, 1), (16, 2, 64, 40, 30), (4, 1, 128, 40, 100),
+                                                   (2, 1, 64, 3000, 200)])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+def test_scores_below_the_range(heads, kv, dim, past, new, scale):
+    """Every score of the last head below -2^128: there is no weight to be had from them, which shows (a NaN or an infinity) instead of
+    passing for zeros.  One tile, tiles cut along their keys and merged, tiles of few columns and of many."""
+    announce(f"scores below the range {heads}/{kv}/{dim} {past}+{new} scale={scale}")
+    m = Model(heads, kv, dim, n_blocks=64, max_seqs=3, max_seq_tokens=3500, max_tokens=4000, seed=past + new)
+    try:
+        n = past + new
+        keys = bf16(m.rng, n, kv, dim)
+        keys[:, -1] = -(keys[:, -1].abs() + 0.5) * 2.0 ** 60
+        keys = keys.reshape(n, kv * dim)
+        if past:
+            m.extend([1], [0], [past])
+            m.store(0, keys[:past])
+        m.extend([1], [past], [new])
+        m.store(0, keys[past:])
+        q = bf16(m.rng, new, heads, dim)
+        q[:, -(heads // kv):] *= 2.0 ** -60                    # (scores of ordinary size for the heads beside it)
+        q[:, -1] = (bf16(m.rng, new, dim).abs() + 0.5) * 2.0 ** 70 * scale
+        got = m.kv.attend(0, q.reshape(new, -1).cuda(), scale).view(new, heads, dim)
+        # the other heads' are what they should be (a column's weights are rounded behind a maximum that its tile's other columns move: no
+        # comparison bit for bit)
+        q64, k64, v64 = f64(q), m.keys[0][1], m.values[0][1]
+        with np.errstate(all="ignore"):
+            ref, size, top = okv.attend(q64, k64, v64, past, scale)
+        split = np.abs(q64).max(axis=2, keepdims=True) * np.repeat(np.abs(k64).sum(axis=2).max(axis=0), heads // kv)[None, :, None]
+        over = np.abs(f64(got) - ref) - attend_bound(ref, size, top, n, dim, split)
+        assert (over[:, :-1] <= 0).all(), float(over[:, :-1].max())
+        assert not torch.isfinite(got[:, -1]).any()
+    finally:
+        m.close()
+
+
+def test_a_score_below_the_range_beside_others_has_no_weight():
+    """Where another key's score is a number, the weight of one below the range is zero, as it should be."""
+    m = Model(2, 1, 64, n_blocks=64, max_seqs=3, max_seq_tokens=3500, max_tokens=4000)
+    try:
+        keys = bf16(m.rng, 3000, 64)
+        keys[100:2700] = -(keys[100:2700].abs() + 0.5) * 2.0 ** 60
+        keys[:100], keys[2700:] = keys[:100] * 2.0 ** -75, keys[2700:] * 2.0 ** -75
+        m.extend([1], [0], [2990])
+        m.store(0, keys[:2990])
+        m.extend([1], [2990], [10])
+        m.store(0, keys[2990:])
+        q = (bf16(m.rng, 10, 128).float().abs() + 0.5) * 2.0 ** 70
+        got = m.kv.attend(0, q.bfloat16().cuda(), 1.0)
+        # what is left: keys 0 .. 99 and 2700 .. , attended by themselves in a second sequence
+        left = torch.cat([torch.arange(100), torch.arange(2700, 3000)])
+        values = m.values[0][1][left.numpy()]
+        m.extend([2], [0], [390])
+        m.store(0, keys[left[:390]], torch.from_numpy(values[:390].reshape(390, 64)).bfloat16())
+        m.extend([2], [390], [10])
+        m.store(0, keys[left[390:]], torch.from_numpy(values[390:].reshape(10, 64)).bfloat16())
+        assert np.array_equal(m.values[0][2], values)          # (four-bit values are their own)
+        want = m.check_attend(0, 1.0, q=q.bfloat16())
+        # both round the same weights and the result once; the pieces' maxima differ, which shifts the weights' bits: two half steps of each
+        size = np.abs(values[:, 0]).max()
+        assert np.abs(f64(got) - f64(want)).max() <= 4 * 2.0 ** -8 * size
     finally:
         m.close()
