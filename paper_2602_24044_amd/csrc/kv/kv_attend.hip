@@ -30,6 +30,11 @@ __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
 
 // Weights may grow to 2^kSlack times those of the running maximum before the sums are scaled down: most blocks then leave them alone.
 constexpr float kSlack = 8.f;
+// A weight is 2^(s scale - m) with the product unrounded and m the rounded product of the largest.  From this maximum on half a step of it
+// is a factor of two, and more further on: the largest key's weight itself would leave the range.  A wave with such a column rounds all
+// products first, and looks at every block as at one that makes m grow (limit -inf), so that the others' blocks do not ask for it (8192 tokens
+// 552 -> 556 us under the profiler; as a question of its own in every block 559).
+constexpr float kFar = 16777216.f;
 
 // The largest over lanes 32 apart, and over lanes 16 and 32 apart: rows of a register change places with rows of its copy on the vector
 // unit.  (The copy is hidden from the compiler, which otherwise takes both results for one and drops the comparison.)
@@ -120,6 +125,7 @@ template <int W> __device__ inline void load_words(uint32_t (&d)[W], const uint8
 // the values), acc[j][i]: dimension E (4 quarter + i) + j of it.
 template <int D> struct Running {
     float m;
+    float limit, by;                                   // a score that makes m grow; what scores are multiplied by: their scale, or 1 (kFar)
     f32x4 l, acc[D / 16];
 };
 
@@ -238,13 +244,19 @@ template <int D> __device__ inline void weights(Running<D>& r, uint32_t (&p)[4][
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
     top = max_quarters(top) * scale;
-    if (__any(top > r.m + kSlack)) {
-        const float m = fmaxf(r.m, top);
-        const float down = exp2_fast(r.m - (m == -INFINITY ? 0.f : m));
+    if (__any(top > r.limit)) {
+        const float m = fmaxf(r.m, top), from = m == -INFINITY ? 0.f : m;
+        const float down = exp2_fast(r.m - from);
+        const bool far = __any(__builtin_fabsf(from) > kFar);
         r.l *= down;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) r.acc[j] *= down;
         r.m = m;
+        r.limit = far ? -INFINITY : m + kSlack;
+        r.by = far ? 1.f : scale;
+        if (far)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) s[t] *= scale;
     }
     // a column that has seen no key yet keeps m = -inf: its weights are 2^-inf = 0, not 2^(-inf + inf)
     const float base = r.m == -INFINITY ? 0.f : r.m;
@@ -252,9 +264,7 @@ template <int D> __device__ inline void weights(Running<D>& r, uint32_t (&p)[4][
     for (int t = 0; t < 4; ++t) {
         float w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            w[i] = exp2_fast(__builtin_fmaf(s[t][i], scale, -base));
-        }
+        for (int i = 0; i < 4; ++i) w[i] = exp2_fast(__builtin_fmaf(s[t][i], r.by, -base));
         p[t][0] = pack_bf16(w[0], w[1]);
         p[t][1] = pack_bf16(w[2], w[3]);
     }
@@ -341,7 +351,8 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
         const int32_t* blocks = a.t.table + (size_t)r.row * a.t.row_blocks + r.block;
         const int n = r.blocks, first = r.block, len = r.len;
         Running<D> run;
-        run.m = -INFINITY;
+        run.m = run.limit = -INFINITY;
+        run.by = scale;
         run.l = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) run.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -532,6 +543,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
         for (int x = 0; x < 16; ++x) o[d][x] = 0.f;
     float m = -INFINITY, l = 0.f;
     const float scale = positive(a.scale_log2);
+    float most = -INFINITY, by = scale;                // as in Running
 
     Raw<D> raw;
     // A block's keys out of LDS, and one of the 4 X products that make its scores.
@@ -600,13 +612,19 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 #pragma unroll
             for (int x = 0; x < 16; ++x) top = fmaxf(top, s[k][x]);
         top = max_halves(top) * scale;
-        if (__any(top > m + kSlack)) {
-            const float grown = fmaxf(m, top);
-            const float down = exp2_fast(m - (grown == -INFINITY ? 0.f : grown));
+        if (__any(top > most)) {
+            const float grown = fmaxf(m, top), from = grown == -INFINITY ? 0.f : grown;
+            const float down = exp2_fast(m - from);
+            const bool far = __any(__builtin_fabsf(from) > kFar);
             l *= down;
 #pragma unroll
             for (int d = 0; d < N; ++d) o[d] *= down;
             m = grown;
+            most = far ? -INFINITY : m + kSlack;
+            by = far ? 1.f : scale;
+            if (far)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) s[k] *= scale;
         }
         const float base = m == -INFINITY ? 0.f : m;
         // The order is pinned here: an MFMA of the next scores (of no use in the last iteration: what is in LDS then are older codes), and in
@@ -631,7 +649,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
 #pragma unroll
             for (int y = P * j; y < P * (j + 1); y += 2) {
                 const int k = y / 16, x = y % 16;
-                const float p0 = exp2_fast(__builtin_fmaf(s[k][x], scale, -base)), p1 = exp2_fast(__builtin_fmaf(s[k][x + 1], scale, -base));
+                const float p0 = exp2_fast(__builtin_fmaf(s[k][x], by, -base)), p1 = exp2_fast(__builtin_fmaf(s[k][x + 1], by, -base));
                 const uint32_t two = pack_bf16(p0, p1);
                 l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
                 w[2 * k + x / 8][(x % 8) / 2] = two;

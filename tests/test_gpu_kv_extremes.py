@@ -129,3 +129,36 @@ def test_a_score_below_the_range_beside_others_has_no_weight():
         assert np.abs(f64(got) - f64(want)).max() <= 4 * 2.0 ** -8 * size
     finally:
         m.close()
+
+
+@pytest.mark.parametrize("power", [20, 27, 33, 45, 80, 116])
+@pytest.mark.parametrize("heads,kv,dim,past,new", [(4, 2, 64, 0, 1), (8, 2, 128, 70, 3), (1, 1, 128, 3000, 1), (4, 1, 128, 40, 100), (1, 1, 64, 3000, 200)])
+def test_large_scores(heads, kv, dim, past, new, power):
+    """Scores so large that their last bit stands for far more than a factor of two in the weights: one key takes all of the weight, and its
+    value comes out.  The scores are sums of few products of few bits, so that they are exact, and one half apart or more."""
+    announce(f"large scores 2^{power} {heads}/{kv}/{dim} {past}+{new}")
+    m = Model(heads, kv, dim, n_blocks=64, max_seqs=3, max_seq_tokens=3500, max_tokens=4000, seed=past + new)
+    try:
+        n = past + new
+        # two dimensions of a key count: a magnitude that the format holds exactly, and which token has the largest
+        keys = torch.zeros(n, kv, dim)
+        level = torch.from_numpy(m.rng.integers(0, 6, size=(n, kv)))
+        keys[:, :, 1] = torch.tensor([0.5, 1.0, 1.5, 2.0, 3.0, 4.0])[level]
+        best = int(m.rng.integers(0, past + 1))
+        keys[best, :, 1] = 6.0                                 # seen by every token of the step
+        keys = keys.reshape(n, kv * dim).bfloat16()
+        values = bf16(m.rng, n, kv * dim)
+        if past:
+            m.extend([1], [0], [past])
+            m.store(0, keys[:past], values[:past])
+        m.extend([1], [past], [new])
+        m.store(0, keys[past:], values[past:])
+        for scale in (1.0, 0.7, -1.3, dim ** -0.5):
+            q = torch.zeros(new, heads, dim)
+            # (odd multiples: the product with scale * log2(e) is not exact, whichever side it is rounded to)
+            q[:, :, 1] = float(np.sign(scale)) * (1 + torch.from_numpy(m.rng.integers(0, 128, size=(new, heads))) / 128) * 2.0 ** power
+            got = f64(m.kv.attend(0, q.reshape(new, -1).bfloat16().cuda(), scale)).reshape(new, heads, dim)
+            want = np.repeat(m.values[0][1][best], heads // kv, axis=0)
+            assert np.array_equal(got, np.broadcast_to(want, got.shape)), (scale, float(np.nanmax(np.abs(got - want))))
+    finally:
+        m.close()
