@@ -433,6 +433,8 @@ def head_norm_rotate(q: Optional[torch.Tensor], k: Optional[torch.Tensor], n_hea
     some, heads = (q, n_heads) if q is not None else (k, n_kv_heads)
     if some is None or some.dim() != 2 or heads < 1 or not some.is_cuda:
         raise ValueError("q or k: bf16 [T, heads * dim] on a GPU expected")
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("an output without its operand")
     T, device, dim = some.shape[0], some.device, some.shape[1] // heads
     with _On(device):
         at = {"q": (None, 0), "k": (None, 0), "q_out": (None, 0), "k_out": (None, 0)}
@@ -543,6 +545,8 @@ class KvCache:
         """The step's keys (normed, rotated) and values into the layer's cache; returns the normed and rotated queries."""
         step, dev = self._current_step(), self.device
         T = step.T
+        if q is None and out is not None:
+            raise ValueError("out: there are no queries to put there")
         with _On(dev):
             at = {"k": (k.data_ptr(), _rows(k, T, self.k_width, dev, "k")), "v": (v.data_ptr(), _rows(v, T, self.k_width, dev, "v"))}
             if q is not None:
