@@ -541,7 +541,7 @@ lora_status lora_kv_release(lora_kv *kv, int32_t n, const int32_t *d_seq, const 
  * heads of a token next to each other; strides count elements from token to token (0: dense; multiples of 8, at
  * least the heads' width), pointers are 16-byte aligned.  Norm (where there is a weight): u = x / sqrt(mean(x^2) + eps) * w over
  * each head.  Rotation (where d_inv_freq is given): the pair p = 0 .. head_dim / 2 - 1 turns by the angle position *
- * d_inv_freq[p], taken in 64 bits.  Sums and products are fp32 (of keys on their way into a cache fp64), of rows with a norm whose
+ * d_inv_freq[p], taken in 64 bits (and below 2^50).  Sums and products are fp32 (of keys on their way into a cache fp64), of rows with a norm whose
  * mean square lies outside of 2^-40 .. 2^40 on values scaled by a power of two, so that rows of any finite values have the norm that the
  * formula gives them (zeros without an eps: NaN); one rounding of the result. */
 typedef struct {
@@ -562,7 +562,7 @@ enum {
 /* Norm and rotation of queries and keys, on the current device: d_q [T, n_heads * head_dim] and d_k [T, n_kv_heads *
  * head_dim] (either may be NULL, then its output too), d_position: device int32[T] (may be NULL without rotation).
  * What lora_kv_store does for a cache, for programs that keep theirs elsewhere.  d_v must be NULL.
- * Errors: INVALID_ARG (null or misaligned pointers, strides, eps, pairing, T < 0), SHAPE (heads, head_dim), HIP. */
+ * Errors: INVALID_ARG (null or misaligned pointers, strides, eps, pairing, T outside of 0 .. 2^20), SHAPE (heads, head_dim), HIP. */
 lora_status lora_head_norm_rotate(int32_t T, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, const int32_t *d_position,
                                   const lora_heads *heads, void *stream);
 
@@ -577,7 +577,7 @@ lora_status lora_kv_store(lora_kv *kv, int32_t layer, const lora_kv_step *step, 
  * keys k <= position[t] of the token's sequence (its own among them: lora_kv_store comes first).  d_q: bf16 [T, n_heads *
  * head_dim], normed and rotated; d_out: the same shape, apart from d_q; strides as in lora_heads.  Keys and values enter as the exact
  * values that their codes stand for; a query's values as bf16 has them, but those below 2^-14 of the head's largest, which may be
- * off by 2^-21 of it.  Scores and sums are fp32 (a score above its range, all of a query's scores below it, or a sum of
+ * off by 2^-21 of it (by 2^-134 where that is more).  Scores and sums are fp32 (a score above its range, all of a query's scores below it, or a sum of
  * values beyond it gives a NaN or an infinity in its head); the weights of the softmax are rounded to bf16, and it is these that their sum counts; one rounding of the result.  A
  * NaN or an infinity in a query makes its own head's row NaN.  Rows of a refused request are set to zero, rows behind the last
  * request are left as they are.  The result does not depend on what else the step holds beyond these roundings, and is the
@@ -589,7 +589,7 @@ lora_status lora_kv_attend(lora_kv *kv, int32_t layer, const lora_kv_step *step,
 /* n tokens out of a layer of the cache, as the bf16 values that their codes stand for (to move a sequence, or to look at
  * it): token d_position[i] of the sequence in row d_seq[i] goes to row i of d_k_out and d_v_out [n, n_kv_heads * head_dim], 16-byte
  * aligned, either may be NULL.  A token outside of the row's blocks sets LORA_KV_FLAG_REFUSED and reads as zeros.  Needs no step.
- * Errors: INVALID_ARG, HIP. */
+ * Errors: INVALID_ARG (also n above 2^24), HIP. */
 lora_status lora_kv_read(lora_kv *kv, int32_t layer, int32_t n, const int32_t *d_seq, const int32_t *d_position, void *d_k_out,
                          void *d_v_out, void *stream);
 

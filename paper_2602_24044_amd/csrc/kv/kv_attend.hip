@@ -32,8 +32,8 @@ __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
 constexpr float kSlack = 8.f;
 // A weight is 2^(s scale - m) with the product unrounded and m the rounded product of the largest.  From this maximum on half a step of it
 // is a factor of two, and more further on: the largest key's weight itself would leave the range.  A wave with such a column rounds all
-// products first, and looks at every block as at one that makes m grow (limit -inf), so that the others' blocks do not ask for it (8192 tokens
-// 552 -> 556 us under the profiler; as a question of its own in every block 559).
+// products first, and looks at every block as at one that makes m grow (limit -inf), so that the others' blocks do not ask for it (a pass over
+// 8192 tokens 517 -> 522 us; with a question of its own in every block half as much again).
 constexpr float kFar = 16777216.f;
 
 // The largest over lanes 32 apart, and over lanes 16 and 32 apart: rows of a register change places with rows of its copy on the vector
@@ -61,7 +61,7 @@ __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // A wave takes a piece of a tile by itself, eleven waves on a CU.  Its blocks are copied to LDS as they are, the next block's keys as
 // soon as this block's scores are there, its values at the end of the block: what is on its way hangs on no register (four waves that
 // share a tile's blocks and fetch them through registers: 91 us instead of 86 for 256 requests; one place for keys and sixteen waves a
-// CU: slower too).  The cache's bytes bound it: those 256 requests (378 MB) at 4.4 TB/s, one of 130000 tokens (141 MB) in 29 us, 4.8
+// CU: slower too).  The cache's bytes bound it: those 256 requests (383 MB) at 4.5 TB/s, one of 130000 tokens (143 MB) in 30 us, 4.8
 // TB/s.  The matrix units are busy for 16 % of that and the vector unit for 37 %; what is missing is that all pieces start at once and the
 // longest end alone.
 template <int D> struct Stage {
@@ -426,7 +426,8 @@ template <int D> __global__ __launch_bounds__(64, 3) void attend_few_kernel(Atte
 // registers, where each thread converts an eighth of 16 tokens to bf16 operands of V^T in LDS, once for all four waves.  Two stages: the next
 // block is made while this one is used.
 //
-// A prompt of 8192 tokens, 32 heads on 8 of 128 (550 GFLOP) takes 490 - 550 us: 1.0 - 1.1 PFLOP/s, where a large bf16 product reaches 1.25.
+// A prompt of 8192 tokens, 32 heads on 8 of 128 (550 GFLOP) takes 485 - 515 us, by the card: 1.07 - 1.13 PFLOP/s, where a large bf16 product
+// reaches 1.25 (heads of 64: 301 us, 0.9).
 // Matrix and vector units are busy for half of the time each, LDS for a third; leaving out any one of them (scores, exponentials,
 // conversion, products with the values) takes 5 - 17 % off, so it is the chain through all of them, twice on each SIMD, that counts.
 // Not kept: 64 columns a wave, alone on its SIMD (694 us: scores and sums change places between the two kinds of registers);
@@ -489,7 +490,7 @@ template <int D> __device__ inline void convert(Tile<D>& t, const Raw<D>& r, con
     }
 }
 
-// A block's keys and their exponents to LDS (lds: where the tile is): 1 KB a wave, the exponents by the first.
+// A block's keys and their exponents to LDS (lds: where the tile is): 1 KB a wave, the exponents by the last of these waves.
 template <int D> __device__ inline void copy_block_keys(uint32_t lds, const uint8_t* part, int wave, int lane)
 {
     constexpr int keys = kBlock * Part<D>::kRow, exps = kBlock * Part<D>::kGroups;
@@ -503,9 +504,9 @@ template <int D> __global__ __launch_bounds__(256, 2) void attend_many_kernel(At
     __shared__ __align__(1024) Tile<D> tiles[2];
     const uint32_t lds = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)tiles;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, h = lane >> 5;
-    // Entries of a request begin with the longest.  Where all of them find room at once, two a CU, the second of a CU is taken from the list's
-    // end, so that long ones share with short ones (a prompt of 2000 tokens 62 -> 57 us, two of 900 39 -> 35); where they do not, the longest
-    // go first and the rest follows as CUs become free.
+    // Entries of a request begin with the longest; requests follow each other as they are.  Where all entries find room at once, two a CU, the
+    // second of a CU is taken from the list's end, so that a request's long ones share with short ones (a prompt of 2000 tokens 54 -> 49 us, two
+    // of 900 34 -> 30; six of 300 - 1000 in no order 48 -> 49); where they do not, the list's order stands and the rest follows as CUs become free.
     const int there = a.t.head->n_many * a.n_kv, at_once = 2 * a.n_cus;
     if ((int)blockIdx.x >= there) return;
     const int item = there <= at_once && (int)blockIdx.x >= a.n_cus ? there - 1 - ((int)blockIdx.x - a.n_cus) : (int)blockIdx.x;

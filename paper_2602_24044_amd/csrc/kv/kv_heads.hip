@@ -5,8 +5,8 @@
 //   y_p = u_p cos a - u_p' sin a,  y_p' = u_p' cos a + u_p sin a,   a = position * f_p,  p' = p + D/2 (or its neighbour)
 //
 // One read and one write of every head, so the copy rate bounds it: 4099 tokens of 28 + 4 heads of 128 with norm, 67 MB, in 14.9 us (4.5
-// TB/s); 8190 tokens of 64 + 8 heads with norm into the cache, 313 MB, in 67 us (4.7 TB/s; the vector unit is busy for half of it), and
-// their keys and values out of it in 16.5.  D / 8 lanes share a head's row, 16 bytes each; the other half of a rotated pair sits D / 16
+// TB/s); 8190 tokens of 64 + 8 heads with norm into the cache, 313 MB, in 65 us (4.8 TB/s; the vector unit is busy for half of it), and
+// their keys and values out of it in 15.8.  D / 8 lanes share a head's row, 16 bytes each; the other half of a rotated pair sits D / 16
 // lanes away.  Angles are taken in 64 bits (a far position times a frequency has few bits left behind the point in 32) once per token and
 // pair, and shared by all heads through LDS.  Keys on the way to four bits are computed in 64 bits throughout and rounded to 32 once: next
 // to a border between two codes an error of 2^-24 would pick the wrong one now and then.
@@ -146,7 +146,7 @@ template <int L> __device__ inline float norm_power(const u32x4 raw, float eps)
 
 // Norm and rotation of one row of D values, eight of them in a lane.  False, to all of the row's lanes alike: computed in 32 bits, and the mean
 // square lies outside of 2^-40 .. 2^40, where squares begin to leave the type's range; y is of no use then, and the row has to be multiplied by
-// its norm_power.  (Costs rows of ordinary size 2 %: 15.2 instead of 14.9 us for the 4099 tokens above.)
+// its norm_power.  (The question costs rows of ordinary size 2 %: a pass over the 4099 tokens above 15.4 instead of 15.0 us.)
 template <int D, typename R, bool SCALED = false>
 __device__ inline bool norm_rotate(const u32x4 raw, bool norm, float eps, const Turn<D, R>& t, bool rotate, bool pairs, R (&y)[8], float power = 1.f)
 {

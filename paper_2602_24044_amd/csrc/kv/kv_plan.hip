@@ -4,7 +4,8 @@
 // takes max(0, w_i - h_i) blocks more: the lowest free ones, request after request.  A free block is a zero bit of `used`; the k-th
 // free one is found by counting.  Everything is a prefix sum over requests or over bitmap words, integer and so the same whatever
 // order the lanes run in.  The work is nothing and the time is latency: reads that hang on each other (row -> blocks held -> bitmap ->
-// table) and barriers.  One launch for decode steps, two otherwise; one token 5.4 us, 32 requests 6.6, 29 prompts of 20462 tokens 8 + 4.
+// table) and barriers.  One launch for decode steps, two otherwise; one token 5.2 us, 32 requests 6.4, 29 prompts of 20462 tokens 7.9 + 4.0,
+// 1000 requests of one token 16 + 4, 4000 of them 49 + 5.
 #include "kv_internal.hpp"
 
 #include <algorithm>
@@ -157,9 +158,9 @@ __device__ inline void write_merge(const Tables& t, const Request& q, int k)
 __device__ inline int32_t* table_row(const Tables& t, const Request& q) { return t.table + (size_t)(q.held >= 0 ? q.row : 0) * t.row_blocks; }
 
 // Steps of up to kSmallThreads requests: a thread per request, which stays in registers (plan_kernel, which goes over lists in memory and
-// has four times the waves at each barrier, takes 11.3 us for one request where this takes 5.9, 14.7 against 9.8 for 256).  Where no
-// request has more than kSmallNew new tokens (so none needs more than one block) the same launch writes everything out: 7.4 us for one
-// request where the second launch makes it 5.9 + 3.3, 11.9 for 256 requests of four tokens where it makes it 9.8 + 4.0.
+// has four times the waves at each barrier, takes 8.8 us for one request where this takes 3.9, 10.0 against 4.6 for 256).  Where no
+// request has more than kSmallNew new tokens (so none needs more than one block) the same launch writes everything out: 5.2 us for one
+// request where the second launch makes it 3.9 + 2.2, 7.5 for 256 requests of four tokens where it makes it 4.6 + 3.2.
 constexpr int kSmallThreads = 256, kSmallNew = 4, kSmallRows = 1024;
 __global__ __launch_bounds__(kSmallThreads) void plan_small_kernel(PlanArgs a)
 {
