@@ -212,8 +212,8 @@ lora_status lora_bucket(lora_ctx *ctx, const int32_t *d_token_adapter, int32_t T
  * Stream ordering: all forward calls (and segment maps) of one context share its scratch (split-K partial tiles,
  * shrink results, the counters of a launch), so they must not overlap in time.  The library sees to that itself:
  * a call whose stream differs from the stream of the context's previous lora_bucket / forward call is ordered
- * behind it with an event before anything is enqueued (the previous call's stream has to exist then).  Calls that should run concurrently need contexts of
- * their own.  When the call uses the shrink inside its launch and lora_poll_device_flags later reports
+ * behind it with an event before anything is enqueued (the previous call's stream has to exist then).  Calls that
+ * should run concurrently need contexts of their own.  When the call uses the shrink inside its launch and lora_poll_device_flags later reports
  * LORA_FLAG_INTERNAL, the outputs written since the previous poll are undefined.
  * Errors: INVALID_ARG (proj out of range, stale seg, null or misaligned pointers), HIP. */
 lora_status lora_layer_forward(lora_ctx *ctx, int32_t proj, const void *d_x, const void *d_W,
@@ -455,10 +455,11 @@ lora_status lora_priority_sorting(int32_t n_adapters, const int32_t *size, const
  * previous call's is ordered behind it with an event, which is recorded then: the previous call's stream has to live until
  * the next call (or until lora_kv_destroy).  While a stream is being captured no event is recorded or waited
  * for, and replays are outside the library: the caller orders a capture and each of its replays with the other calls
- * on that cache (two graphs of one cache must not run at the same time).  While the stream of the latest call made outside of a
- * capture is being captured, a call on another stream that is not cannot wait for it: INVALID_ARG.  A captured call reads the lengths, rows and
- * tables that are there when it is replayed, but keeps T, n and max_new of the capture: the step in force at a replay is
- * one of the same three (requests without new tokens and rows behind the last request make a smaller one).
+ * on that cache (two graphs of one cache must not run at the same time).  While the stream of the latest call made
+ * outside of a capture is being captured, a call on another stream that is not cannot wait for it: INVALID_ARG.  A captured
+ * call reads the lengths, rows and tables that are there when it is replayed, but keeps T, n and max_new of the capture:
+ * the step in force at a replay is one of the same three (requests without new tokens and rows behind the last request
+ * make a smaller one).
  * ------------------------------------------------------------------------------------------------------------- */
 #define LORA_KV_BLOCK 64
 
@@ -506,8 +507,8 @@ typedef struct {
 size_t lora_kv_slab_bytes(const lora_kv_config *cfg);
 
 /* Creates an empty cache on the current device (paper Sec. 2.1).  Waits for the device (the slab may come from a use whose
- * last work is still queued), sets the whole cache to zero and waits for that.  Calls on one cache are not thread-safe.  Errors: INVALID_ARG (null, out of range, misaligned slab), SHAPE (heads,
- * head_dim), OOM (slab too small), HIP. */
+ * last work is still queued), sets the whole cache to zero and waits for that.  Calls on one cache are not thread-safe.
+ * Errors: INVALID_ARG (null, out of range, misaligned slab), SHAPE (heads, head_dim), OOM (slab too small), HIP. */
 lora_status lora_kv_create(const lora_kv_config *cfg, lora_kv **out);
 
 /* Waits for the cache's device and ends the cache; the slab stays the caller's.  Errors: INVALID_ARG (NULL). */
@@ -526,8 +527,8 @@ lora_status lora_kv_destroy(lora_kv *kv);
  * sequence would exceed max_seq_tokens, d_len is not covered by blocks that the row holds, or its rows do not fit T.  Free
  * blocks are handed out in order until a request does not get all that it needs: it and all later requests that
  * need one get none and are refused (LORA_KV_FLAG_EXHAUSTED).
- * Errors: INVALID_ARG (n or T out of range, max_new < 0, null pointers), HIP (a launch that fails ends the step before: blocks that
- * were on their way to a request may then be lost to the pool). */
+ * Errors: INVALID_ARG (n or T out of range, max_new < 0, null pointers), HIP (a launch that fails ends the step before:
+ * blocks that were on their way to a request may then be lost to the pool). */
 lora_status lora_kv_extend(lora_kv *kv, int32_t n, const int32_t *d_seq, const int32_t *d_len, const int32_t *d_new, int32_t T,
                            int32_t max_new, lora_kv_step *out, void *stream);
 
@@ -541,9 +542,9 @@ lora_status lora_kv_release(lora_kv *kv, int32_t n, const int32_t *d_seq, const 
  * heads of a token next to each other; strides count elements from token to token (0: dense; multiples of 8, at
  * least the heads' width), pointers are 16-byte aligned.  Norm (where there is a weight): u = x / sqrt(mean(x^2) + eps) * w over
  * each head.  Rotation (where d_inv_freq is given): the pair p = 0 .. head_dim / 2 - 1 turns by the angle position *
- * d_inv_freq[p], taken in 64 bits (and below 2^50).  Sums and products are fp32 (of keys on their way into a cache fp64), of rows with a norm whose
- * mean square lies outside of 2^-40 .. 2^40 on values scaled by a power of two, so that rows of any finite values have the norm that the
- * formula gives them (zeros without an eps: NaN); one rounding of the result. */
+ * d_inv_freq[p], taken in 64 bits (and below 2^50).  Sums and products are fp32 (of keys on their way into a cache fp64), of
+ * rows with a norm whose mean square lies outside of 2^-40 .. 2^40 on values scaled by a power of two, so that rows of any
+ * finite values have the norm that the formula gives them (zeros without an eps: NaN); one rounding of the result. */
 typedef struct {
     const void *d_q, *d_k, *d_v;
     int64_t q_stride, k_stride, v_stride;
@@ -577,11 +578,11 @@ lora_status lora_kv_store(lora_kv *kv, int32_t layer, const lora_kv_step *step, 
  * keys k <= position[t] of the token's sequence (its own among them: lora_kv_store comes first).  d_q: bf16 [T, n_heads *
  * head_dim], normed and rotated; d_out: the same shape, apart from d_q; strides as in lora_heads.  Keys and values enter as the exact
  * values that their codes stand for; a query's values as bf16 has them, but those below 2^-14 of the head's largest, which may be
- * off by 2^-21 of it (by 2^-134 where that is more).  Scores and sums are fp32 (a score above its range, all of a query's scores below it, or a sum of
- * values beyond it gives a NaN or an infinity in its head); the weights of the softmax are rounded to bf16, and it is these that their sum counts; one rounding of the result.  A
- * NaN or an infinity in a query makes its own head's row NaN.  Rows of a refused request are set to zero, rows behind the last
- * request are left as they are.  The result does not depend on what else the step holds beyond these roundings, and is the
- * same from call to call.
+ * off by 2^-21 of it (by 2^-134 where that is more).  Scores and sums are fp32 (a score above its range, all of a query's
+ * scores below it, or a sum of values beyond it gives a NaN or an infinity in its head); the weights of the softmax are rounded
+ * to bf16, and it is these that their sum counts; one rounding of the result.  A NaN or an infinity in a query makes its own
+ * head's row NaN.  Rows of a refused request are set to zero, rows behind the last request are left as they are.  The result
+ * does not depend on what else the step holds beyond these roundings, and is the same from call to call.
  * Errors: INVALID_ARG (layer, stale step, null or misaligned pointers, strides, scale not finite), HIP. */
 lora_status lora_kv_attend(lora_kv *kv, int32_t layer, const lora_kv_step *step, float scale, const void *d_q, int64_t q_stride,
                            void *d_out, int64_t out_stride, void *stream);

@@ -33,7 +33,7 @@ constexpr float kSlack = 8.f;
 // A weight is 2^(s scale - m) with the product unrounded and m the rounded product of the largest.  From this maximum on half a step of it
 // is a factor of two, and more further on: the largest key's weight itself would leave the range.  A wave with such a column rounds all
 // products first, and looks at every block as at one that makes m grow (limit -inf), so that the others' blocks do not ask for it (a pass over
-// 8192 tokens 517 -> 522 us; with a question of its own in every block half as much again).
+// 8192 tokens 517 -> 522 us; with a question of its own in every block another 3 - 4).
 constexpr float kFar = 16777216.f;
 
 // The largest over lanes 32 apart, and over lanes 16 and 32 apart: rows of a register change places with rows of its copy on the vector
